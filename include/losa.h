@@ -31,7 +31,9 @@
  *     throws or aborts.  Device-side indices (page ids, token ids) outside their range
  *     are skipped by the kernels, never dereferenced.
  *   - Calls on one losa_ctx share its workspace: issue them on one stream, or
- *     serialise them.
+ *     serialise them.  (losa_rotate, losa_append_kv, losa_append_packed and losa_read_packed use no workspace.)
+ *   - A cache is held in T (losa_kv) or in 4 bits a number (losa_packed_kv).  losa_append_kv / losa_append_packed fill
+ *     pages, losa_sparse_attn / losa_sparse_attn_packed and losa_step / losa_step_packed read them.
  */
 #ifndef LOSA_H
 #define LOSA_H
@@ -274,6 +276,103 @@ typedef enum {
 } losa_tuning;
 losa_status losa_set_tuning(losa_ctx* ctx, losa_tuning knob, int64_t value);
 
+/* ---- New tokens: position rotation, and their way into a cache's pages ---- */
+
+/* Rotary position embedding.  Angle i of position p has cosine cos_sin[p][i] and sine cos_sin[p][rotary_dim/2 + i], whatever rule made
+ * them; it turns (x1, x2) into (x1 cos - x2 sin, x2 cos + x1 sin), where (x1, x2) are the channels
+ *   LOSA_ROTATE_HALVES : (i, i + rotary_dim/2)        LOSA_ROTATE_PAIRS : (2 i, 2 i + 1)
+ * Channels from rotary_dim on pass through.  Results are the exact ones of the given numbers, rounded once to T. */
+typedef enum { LOSA_ROTATE_HALVES = 0, LOSA_ROTATE_PAIRS = 1 } losa_rotation_style;
+typedef struct {
+  const float* cos_sin;   /* float [max_positions, rotary_dim], 16-byte aligned */
+  int32_t max_positions;  /* host: rows of the table; a token at a position outside it is left out, as other indices are */
+  int32_t rotary_dim;     /* host: a multiple of 16, up to d */
+  int32_t style;          /* host: losa_rotation_style */
+} losa_rotation;
+
+/* Turns the query and key rows of `tokens` tokens, the block's of a step for instance.
+ *   positions       : int32 [tokens]; rows of a token whose position is outside the table are not written
+ *   q, q_out        : T [tokens, Hq, d], consecutive tokens *_stride elements apart (0: Hq*d).  q_out may be q with its stride
+ *   k, k_out        : T [tokens, Hkv, d], likewise; either pair may be NULL
+ * Rows are 16-byte aligned: the pointers and, in bytes, the strides. */
+losa_status losa_rotate(losa_ctx* ctx, void* stream, const losa_rotation* rotation, const int32_t* positions, int32_t tokens,
+                        const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                        const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride);
+
+/* Tokens that join a cache: a prompt's, a finished block's, the one just decoded. */
+typedef struct {
+  const void* k;              /* T [num_tokens, Hkv, d], consecutive tokens k_stride elements apart (0: Hkv*d): a part of a fused
+                                 projection's output will do.  16-byte aligned rows, as in losa_rotate */
+  const void* v;              /* the same, v_stride */
+  int64_t k_stride, v_stride;
+  const int32_t* tok_indptr;  /* [batch+1] rows tok_indptr[b] .. tok_indptr[b+1]-1 of k and v join sequence b */
+  const int32_t* positions;   /* nullable [num_tokens]: positions for the rotation; NULL: a token's place in its sequence */
+  int32_t num_tokens;         /* host: rows of k and v (0: nothing is done) */
+  int32_t max_new_tokens;     /* host: an upper bound on the tokens that join any one sequence, if the caller knows one (the grid
+                                 is sized by it), else 0.  Tokens beyond the bound may be left out */
+} losa_new_tokens;
+
+/* Writes new tokens into the pages of a cache: keys, turned first if `rotation` is not NULL, token-major, values channel-major, and the
+ * bounds of every page that gets a token (kv->meta; NULL: none are kept), so that losa_page_bounds need not be called
+ * for them.
+ *   kv->seq_lens[b] : the length WITH the new tokens: they take the last tok_indptr[b+1] - tok_indptr[b] places
+ * Where the first of them is not the first token of its page, the page's bounds have to hold those of the tokens before it.
+ * Slots that get no token keep what they hold.  Tokens whose page is not listed, not in the pool or beyond max_seq_pages, or that the
+ * rotation's table does not reach, are left out.  A page that gets tokens belongs to one sequence. */
+losa_status losa_append_kv(losa_ctx* ctx, void* stream, const losa_kv* kv, const losa_new_tokens* fresh,
+                           const losa_rotation* rotation);
+
+/* ---- A cache in 4 bits a number ---- */
+
+/* The OCP microscaling format MXFP4 (E2M1 codes, E8M0 scales): 4.25 bits a number.  A token's key (value) of one KV head is cut
+ * into groups of 32 channels; a group has a scale X = 2^(byte - 127) and a code of 4 bits per channel: a sign and one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 times X.  losa_append_packed picks X so that the group's largest magnitude is in [3.5 X, 7 X) and
+ * rounds to nearest, ties to the even code: an error of up to a fifth of a number from X on, and of up to X / 4 below.
+ * The scale bytes stay in 2..252 for keys and in 105..140 for values, which are then exact in bfloat16 and in half precision (values:
+ * multiples of 2^-23 up to 49152, where they saturate); a group that holds an infinity or a NaN gets the byte 255 and reads as
+ * NaN.  Pages filled in another way have to keep to these bytes too.
+ * The page table, the lengths and the metadata are losa_kv's; the bounds are those of the numbers the codes stand for, so that they bound
+ * what the attention sees.  losa_score_pages and losa_score_pages_shared, which look at nothing else, take a losa_kv with the code pools in
+ * the place of k_pages and v_pages. */
+typedef struct {
+  void* k_codes;          /* uint8 [num_pages, Hkv, g, d/2]: byte i of a token holds channels 2i (low four bits) and 2i+1 */
+  void* v_codes;          /* uint8 [num_pages, Hkv, g/4, 16, d/32, 4]: byte [q][r][j][t] holds channels 32j+r (low four bits) and 32j+16+r
+                             of token 4q+t of the page */
+  void* scales;           /* uint8 [num_pages, Hkv, 2, g, d/32]: bytes of the keys' groups, then of the values' */
+  void* meta;             /* T [num_pages, Hkv, 2, d], as in losa_kv */
+  const int32_t* page_indptr;
+  const int32_t* page_indices;
+  const int32_t* seq_lens;
+  int32_t batch;
+  int32_t num_pages;
+  int32_t max_seq_pages;
+} losa_packed_kv;         /* (pools 16-byte aligned) */
+
+/* losa_append_kv into a 4-bit cache.  A key is turned and rounded to T first, as a cache of T would hold it, then packed. */
+losa_status losa_append_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, const losa_new_tokens* fresh,
+                               const losa_rotation* rotation);
+
+/* The numbers of a cache's last tokens, the way losa_append_packed takes them: of sequence b its last
+ * tok_indptr[b+1] - tok_indptr[b] tokens (all of them, for a sequence that moves to another cache).
+ *   k_out, v_out : T [num_tokens, Hkv, d]; either may be NULL.  Rows of tokens that are left out (as in losa_append_kv) are not written
+ *   max_tokens   : host: an upper bound on the tokens read of any one sequence, or 0 */
+losa_status losa_read_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, const int32_t* tok_indptr, int32_t num_tokens,
+                             int32_t max_tokens, void* k_out, void* v_out);
+
+/* losa_sparse_attn over a 4-bit cache: the same arguments and results, for one query row per KV head to B*G of them.  Against
+ * exact attention over the numbers the codes stand for: products accumulate in float, probabilities enter the value product with 22 bits;
+ * relative error of o_p some 1e-6 in both modes (T is the type of q; float queries keep their 24 bits). */
+losa_status losa_sparse_attn_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, const void* q,
+                                    const int32_t* active_idx, const int32_t* active_count,
+                                    const int32_t* sel_pages, const int32_t* sel_count, int32_t cap,
+                                    void* o_p, float* lse_p);
+
+/* losa_step over a 4-bit cache: the same arguments and results. */
+losa_status losa_step_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, int32_t step_index,
+                             const void* h_cur, const void* h_prev, const void* q,
+                             losa_select_mode mode, float param, int32_t topk_pages,
+                             void* o_p, float* lse_p, uint8_t* mask, int32_t* sel_count);
+
 /* Measurement hooks (the paper's latency breakdown names four components: criticality
  * estimation, locality pruning, cache management, attention computation; cache management
  * costs nothing here because reuse is "do not write").  While enabled, every launch made
@@ -289,8 +388,8 @@ typedef enum {
   LOSA_STAGE_TOPK = 2,     /* top-k + union kernels                    ("criticality estimation") */
   LOSA_STAGE_ATTN = 3,     /* split-K attention kernel                 ("attention computation") */
   LOSA_STAGE_MERGE = 4,    /* split-K merge kernel                     ("attention computation") */
-  LOSA_STAGE_BOUNDS = 5,   /* page min/max kernel (once per block) */
-  LOSA_STAGE_BLOCK = 6,    /* in-block attention + final merge kernel */
+  LOSA_STAGE_BOUNDS = 5,   /* what keeps pages: min/max kernel (once per block), new tokens into pages and out of them */
+  LOSA_STAGE_BLOCK = 6,    /* in-block attention + final merge kernel, rotation */
   LOSA_NUM_STAGES = 7
 } losa_stage;
 losa_status losa_profile_enable(losa_ctx* ctx, int32_t enable);

@@ -19,9 +19,11 @@ LOSA_SEL_TOPK, LOSA_SEL_FRACTION, LOSA_SEL_THRESHOLD, LOSA_SEL_MASS = 0, 1, 2, 3
 EXPORTS = ["losa_workspace_bytes", "losa_create", "losa_destroy", "losa_last_error", "losa_select_active",
            "losa_page_bounds", "losa_score_pages", "losa_sparse_attn", "losa_step", "losa_profile_enable",
            "losa_profile_read", "losa_calibration_copy", "losa_block_merge", "losa_score_pages_shared",
-           "losa_select_active_static", "losa_set_tuning", "losa_calibration_read"]
+           "losa_select_active_static", "losa_set_tuning", "losa_calibration_read", "losa_rotate", "losa_append_kv",
+           "losa_append_packed", "losa_read_packed", "losa_sparse_attn_packed", "losa_step_packed"]
 (LOSA_TUNE_ATTN_WORKGROUPS, LOSA_TUNE_SELECT_ROUND, LOSA_TUNE_SCORE_ROUND, LOSA_TUNE_RANK_IN_SCORES,
  LOSA_TUNE_UNION_IN_ATTENTION, LOSA_TUNE_SHARED_TILES, LOSA_TUNE_HALF_PRECISION_VALUES) = range(7)
+LOSA_ROTATE_HALVES, LOSA_ROTATE_PAIRS = 0, 1
 STAGES = ["locality", "score", "topk", "attn", "merge", "bounds", "block"]
 
 
@@ -43,6 +45,21 @@ class losa_kv(C.Structure):
     _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("meta", C.c_void_p),
                 ("page_indptr", C.c_void_p), ("page_indices", C.c_void_p), ("seq_lens", C.c_void_p),
                 ("batch", C.c_int32), ("num_pages", C.c_int32), ("max_seq_pages", C.c_int32)]
+
+
+class losa_packed_kv(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("scales", C.c_void_p), ("meta", C.c_void_p),
+                ("page_indptr", C.c_void_p), ("page_indices", C.c_void_p), ("seq_lens", C.c_void_p),
+                ("batch", C.c_int32), ("num_pages", C.c_int32), ("max_seq_pages", C.c_int32)]
+
+
+class losa_rotation(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("max_positions", C.c_int32), ("rotary_dim", C.c_int32), ("style", C.c_int32)]
+
+
+class losa_new_tokens(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("tok_indptr", C.c_void_p), ("positions", C.c_void_p), ("num_tokens", C.c_int32), ("max_new_tokens", C.c_int32)]
 
 
 _lib = None
@@ -87,6 +104,19 @@ def load_library() -> C.CDLL:
     lib.losa_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
     lib.losa_block_merge.restype = C.c_int
     lib.losa_block_merge.argtypes = [vp, vp, i32, p, p, p, p, p, p, p, p]
+    i64, pk, rot, new = C.c_int64, C.POINTER(losa_packed_kv), C.POINTER(losa_rotation), C.POINTER(losa_new_tokens)
+    lib.losa_rotate.restype = C.c_int
+    lib.losa_rotate.argtypes = [vp, vp, rot, p, i32, p, i64, p, i64, p, i64, p, i64]
+    lib.losa_append_kv.restype = C.c_int
+    lib.losa_append_kv.argtypes = [vp, vp, C.POINTER(losa_kv), new, rot]
+    lib.losa_append_packed.restype = C.c_int
+    lib.losa_append_packed.argtypes = [vp, vp, pk, new, rot]
+    lib.losa_read_packed.restype = C.c_int
+    lib.losa_read_packed.argtypes = [vp, vp, pk, p, i32, i32, p, p]
+    lib.losa_sparse_attn_packed.restype = C.c_int
+    lib.losa_sparse_attn_packed.argtypes = [vp, vp, pk, p, p, p, p, p, i32, p, p]
+    lib.losa_step_packed.restype = C.c_int
+    lib.losa_step_packed.argtypes = [vp, vp, pk, i32, p, p, p, C.c_int, f32, i32, p, p, p, p]
     lib.losa_calibration_copy.restype = C.c_int
     lib.losa_calibration_copy.argtypes = [vp, vp, C.c_size_t, vp]
     lib.losa_calibration_read.restype = C.c_int
@@ -132,6 +162,36 @@ class PagedKV:
     def as_struct(self) -> losa_kv:
         return losa_kv(_ptr(self.k_pages), _ptr(self.v_pages), _ptr(self.meta), _ptr(self.page_indptr),
                        _ptr(self.page_indices), _ptr(self.seq_lens), self.batch, self.num_pages, self.max_seq_pages)
+
+
+class PackedKV:
+    """Device tensors of one layer's prefix cache in 4 bits (uint8 pools) plus the host-side counts."""
+
+    def __init__(self, k_codes, v_codes, scales, meta, page_indptr, page_indices, seq_lens, max_seq_pages: int = 0):
+        self.k_codes, self.v_codes, self.scales, self.meta = k_codes, v_codes, scales, meta
+        self.page_indptr, self.page_indices, self.seq_lens = page_indptr, page_indices, seq_lens
+        self.batch = int(seq_lens.numel())
+        self.num_pages = int(k_codes.shape[0])
+        self.max_seq_pages = int(max_seq_pages)
+
+    def as_struct(self) -> losa_packed_kv:
+        return losa_packed_kv(_ptr(self.k_codes), _ptr(self.v_codes), _ptr(self.scales), _ptr(self.meta), _ptr(self.page_indptr),
+                              _ptr(self.page_indices), _ptr(self.seq_lens), self.batch, self.num_pages, self.max_seq_pages)
+
+    def for_scoring(self) -> PagedKV:
+        """The cache as losa_score_pages and losa_score_pages_shared take it: they read its page table and bounds only."""
+        return PagedKV(self.k_codes, self.v_codes, self.meta, self.page_indptr, self.page_indices, self.seq_lens, self.max_seq_pages)
+
+
+class Rotation:
+    """A rotation's table (float32 [positions, rotary_dim]: cosines, then sines) and which channels make a pair."""
+
+    def __init__(self, cos_sin, style: int = LOSA_ROTATE_HALVES):
+        self.cos_sin, self.style = cos_sin, int(style)
+        self.max_positions, self.rotary_dim = int(cos_sin.shape[0]), int(cos_sin.shape[1])
+
+    def as_struct(self) -> losa_rotation:
+        return losa_rotation(_ptr(self.cos_sin), self.max_positions, self.rotary_dim, self.style)
 
 
 class Context:
@@ -240,6 +300,90 @@ def losa_step(ctx: Context, kv: PagedKV, step_index: int, h_cur, h_prev, q, mode
     _check(ctx, load_library().losa_step(ctx.handle, _stream(stream), C.byref(s), step_index, _ptr(h_cur),
                                         _ptr(h_prev), _ptr(q), mode, param, topk_pages, _ptr(o_p), _ptr(lse_p),
                                         _ptr(mask), _ptr(sel_count)))
+
+
+def _row_stride(t, ctx: Context, heads: int, what: str) -> int:
+    """Elements between consecutive tokens of a [tokens, heads, d] tensor of the context's type, whose heads have to lie together."""
+    cfg = ctx.cfg
+    d = cfg.head_dim
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.element_size() != (2 if cfg.dtype == LOSA_BF16 else 4):
+        raise LosaError(LOSA_ERR_INVALID_ARG, f"{what} is not a [tokens, {heads}, {d}] tensor of the context's type")
+    if t.shape[0] == 0:
+        return 0
+    row, head, channel = t.stride()
+    if channel != 1 or (head != d and heads > 1):
+        raise LosaError(LOSA_ERR_INVALID_ARG, f"{what}: the heads of a token do not lie one behind the other")
+    if t.shape[0] == 1:
+        return 0
+    if row == 0:
+        raise LosaError(LOSA_ERR_INVALID_ARG, f"{what}: all tokens are the same row")
+    return row
+
+
+def _same(what: str, *sizes: int) -> int:
+    if len(set(sizes)) > 1:
+        raise LosaError(LOSA_ERR_INVALID_ARG, f"{what}: {sizes} tokens do not agree")
+    return sizes[0]
+
+
+def losa_rotate(ctx: Context, rotation: Rotation, positions, q=None, q_out=None, k=None, k_out=None, stream=None):
+    """q [tokens, Hq, d] and / or k [tokens, Hkv, d], turned by the positions (int32 [tokens]) into q_out / k_out (the inputs
+    themselves, if need be)."""
+    Hq, Hkv = ctx.cfg.num_q_heads, ctx.cfg.num_kv_heads
+    strides = [0 if t is None else _row_stride(t, ctx, h, w) for t, h, w in
+               ((q, Hq, "q"), (q_out, Hq, "q_out"), (k, Hkv, "k"), (k_out, Hkv, "k_out"))]
+    tokens = _same("losa_rotate", int(positions.numel()), *(int(t.shape[0]) for t in (q, q_out, k, k_out) if t is not None))
+    r = rotation.as_struct()
+    _check(ctx, load_library().losa_rotate(ctx.handle, _stream(stream), C.byref(r), _ptr(positions), tokens, _ptr(q), strides[0],
+                                          _ptr(q_out), strides[1], _ptr(k), strides[2], _ptr(k_out), strides[3]))
+
+
+def _new_tokens(ctx: Context, k, v, tok_indptr, positions, max_new_tokens: int) -> losa_new_tokens:
+    h = ctx.cfg.num_kv_heads
+    n = _same("new tokens", int(k.shape[0]), int(v.shape[0]), *(() if positions is None else (int(positions.numel()),)))
+    return losa_new_tokens(_ptr(k), _ptr(v), _row_stride(k, ctx, h, "k"), _row_stride(v, ctx, h, "v"), _ptr(tok_indptr), _ptr(positions),
+                           n, max_new_tokens)
+
+
+def losa_append_kv(ctx: Context, kv: PagedKV, k, v, tok_indptr, rotation: Optional[Rotation] = None, positions=None,
+                   max_new_tokens: int = 0, stream=None):
+    """Tokens k, v [tokens, Hkv, d] (row strides as they are) into the pages and bounds of `kv`, whose seq_lens count them already."""
+    s, n, r = kv.as_struct(), _new_tokens(ctx, k, v, tok_indptr, positions, max_new_tokens), rotation and rotation.as_struct()
+    _check(ctx, load_library().losa_append_kv(ctx.handle, _stream(stream), C.byref(s), C.byref(n), C.byref(r) if r else None))
+
+
+def losa_append_packed(ctx: Context, kv: PackedKV, k, v, tok_indptr, rotation: Optional[Rotation] = None, positions=None,
+                       max_new_tokens: int = 0, stream=None):
+    """The same into a 4-bit cache."""
+    s, n, r = kv.as_struct(), _new_tokens(ctx, k, v, tok_indptr, positions, max_new_tokens), rotation and rotation.as_struct()
+    _check(ctx, load_library().losa_append_packed(ctx.handle, _stream(stream), C.byref(s), C.byref(n), C.byref(r) if r else None))
+
+
+def losa_read_packed(ctx: Context, kv: PackedKV, tok_indptr, k_out, v_out, max_tokens: int = 0, stream=None):
+    """The last tokens of every sequence of a 4-bit cache into k_out / v_out [tokens, Hkv, d] (contiguous; either may be None)."""
+    outs = [t for t in (k_out, v_out) if t is not None]
+    for t in outs:
+        if _row_stride(t, ctx, ctx.cfg.num_kv_heads, "an output") and not t.is_contiguous():
+            raise LosaError(LOSA_ERR_INVALID_ARG, "outputs are contiguous")
+    tokens = _same("outputs", *(int(t.shape[0]) for t in outs)) if outs else 0
+    s = kv.as_struct()
+    _check(ctx, load_library().losa_read_packed(ctx.handle, _stream(stream), C.byref(s), _ptr(tok_indptr), tokens, max_tokens, _ptr(k_out),
+                                               _ptr(v_out)))
+
+
+def losa_sparse_attn_packed(ctx: Context, kv: PackedKV, q, active_idx, active_count, sel_pages, sel_count, cap: int, o_p, lse_p,
+                            stream=None):
+    s = kv.as_struct()
+    _check(ctx, load_library().losa_sparse_attn_packed(ctx.handle, _stream(stream), C.byref(s), _ptr(q), _ptr(active_idx),
+                                                      _ptr(active_count), _ptr(sel_pages), _ptr(sel_count), cap, _ptr(o_p),
+                                                      _ptr(lse_p)))
+
+
+def losa_step_packed(ctx: Context, kv: PackedKV, step_index: int, h_cur, h_prev, q, mode: int, param: float, topk_pages: int, o_p, lse_p,
+                     mask=None, sel_count=None, stream=None):
+    s = kv.as_struct()
+    _check(ctx, load_library().losa_step_packed(ctx.handle, _stream(stream), C.byref(s), step_index, _ptr(h_cur), _ptr(h_prev), _ptr(q),
+                                               mode, param, topk_pages, _ptr(o_p), _ptr(lse_p), _ptr(mask), _ptr(sel_count)))
 
 
 def losa_set_tuning(ctx: Context, knob: int, value: int):

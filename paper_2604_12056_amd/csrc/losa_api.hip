@@ -269,6 +269,59 @@ KvView view_of(const losa_kv* kv, int max_seq_pages) {
   return v;
 }
 
+bool unaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+
+// A packed cache's page table and metadata, checked and seen as a losa_kv's.
+losa_status check_packed(losa_ctx* ctx, const losa_packed_kv* kv, bool need_meta, int* max_seq_pages, KvView* view, PackedView* pk) {
+  if (!kv) return fail(ctx, LOSA_ERR_INVALID_ARG, "kv is NULL");
+  const losa_kv plain{kv->k_codes, kv->v_codes, kv->meta, kv->page_indptr, kv->page_indices, kv->seq_lens, kv->batch, kv->num_pages, kv->max_seq_pages};
+  const losa_status s = check_kv(ctx, &plain, need_meta, max_seq_pages);
+  if (s != LOSA_OK) return s;
+  if (!kv->scales) return fail(ctx, LOSA_ERR_INVALID_ARG, "kv.scales is NULL");
+  if (unaligned(kv->k_codes) || unaligned(kv->v_codes) || unaligned(kv->scales) || unaligned(kv->meta))
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "kv has a pool that is not 16-byte aligned");
+  *view = view_of(&plain, *max_seq_pages);
+  *pk = {(uint8_t*)kv->k_codes, (uint8_t*)kv->v_codes, (uint8_t*)kv->scales};
+  return LOSA_OK;
+}
+
+// A rotation's description (NULL: none, where that is allowed).
+losa_status check_rotation(losa_ctx* ctx, const losa_rotation* r, Rotation* out) {
+  *out = {nullptr, 0, 0, 0};
+  if (!r) return LOSA_OK;
+  if (!r->cos_sin || unaligned(r->cos_sin)) return fail(ctx, LOSA_ERR_INVALID_ARG, "rotation.cos_sin is NULL or not 16-byte aligned");
+  if (r->max_positions < 1) return fail(ctx, LOSA_ERR_INVALID_ARG, "rotation.max_positions must be >= 1");
+  if (r->rotary_dim < 1 || r->rotary_dim > ctx->sh.d)
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "rotation.rotary_dim %d outside 1..head_dim (%d)", r->rotary_dim, ctx->sh.d);
+  if (r->rotary_dim % 16 != 0) return fail(ctx, LOSA_ERR_UNSUPPORTED, "rotation.rotary_dim must be a multiple of 16");
+  if (r->style != LOSA_ROTATE_HALVES && r->style != LOSA_ROTATE_PAIRS)
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "unknown rotation style %d", r->style);
+  *out = {r->cos_sin, r->max_positions, r->rotary_dim, r->style == LOSA_ROTATE_PAIRS};
+  return LOSA_OK;
+}
+
+// The distance between consecutive tokens' rows of `heads` heads, in elements; 0 if `given` is none.
+long row_stride(const losa_ctx* ctx, int64_t given, int heads) {
+  const long dense = (long)heads * ctx->sh.d;
+  if (given == 0) return dense;
+  const int per16 = ctx->cfg.dtype == LOSA_BF16 ? 8 : 4;
+  return given < dense || given % per16 != 0 ? 0 : (long)given;
+}
+
+losa_status check_new(losa_ctx* ctx, const losa_new_tokens* fresh, NewTokens* in, int* max_new) {
+  if (!fresh) return fail(ctx, LOSA_ERR_INVALID_ARG, "the new tokens' description is NULL");
+  if (fresh->num_tokens < 0 || fresh->max_new_tokens < 0)
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "num_tokens and max_new_tokens must be >= 0");
+  *max_new = fresh->max_new_tokens > 0 && fresh->max_new_tokens < fresh->num_tokens ? fresh->max_new_tokens : fresh->num_tokens;
+  if (fresh->num_tokens == 0) return LOSA_OK;
+  if (!fresh->k || !fresh->v || !fresh->tok_indptr) return fail(ctx, LOSA_ERR_INVALID_ARG, "the new tokens have a NULL device pointer");
+  const long ks = row_stride(ctx, fresh->k_stride, ctx->sh.Hkv), vs = row_stride(ctx, fresh->v_stride, ctx->sh.Hkv);
+  if (unaligned(fresh->k) || unaligned(fresh->v) || !ks || !vs)
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "the new tokens' rows overlap or are not 16-byte aligned");
+  *in = {fresh->k, fresh->v, ks, vs, fresh->tok_indptr, fresh->positions, fresh->num_tokens};
+  return LOSA_OK;
+}
+
 losa_status hip_fail(losa_ctx* ctx, const char* what, hipError_t e) {
   return fail(ctx, LOSA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
@@ -456,6 +509,112 @@ losa_status sparse_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, in
   e = launch_attn_merge(st, kv, ctx->sh, batch, in, mfma, nchunk, part, o_p, lse_p, hinted ? rows_upper : 0, few_tile, many_tile);
   if (e != hipSuccess) return hip_fail(ctx, "attn_merge launch", e);
   return LOSA_OK;
+}
+
+// The same over a 4-bit cache.
+losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, const PackedView& pk, int batch, int max_seq_pages, const void* q,
+                             const int32_t* active_idx, const int32_t* active_count, const int32_t* sel_pages, const int32_t* sel_count,
+                             int cap, int rows_upper, float* o_p, float* lse_p, int topk = 0) {
+  const int upper = sel_pages ? (cap < max_seq_pages ? cap : max_seq_pages) : max_seq_pages;
+  if (!active_idx) rows_upper = ctx->sh.rows_max;
+  const bool known = rows_upper >= 1 && rows_upper <= ctx->sh.rows_max;
+  if (!known) rows_upper = ctx->sh.rows_max;
+  Partials part = ctx->part;
+  part.rows = known ? std::min((rows_upper + 15) / 16 * 16, ctx->sh.rows_max) : ctx->sh.rows_max;
+  // (a count that only the device knows is mostly that of a few active tokens: shares as for one block of rows)
+  const int block = packed_block_rows(ctx->cfg.dtype), row_blocks = known ? (rows_upper + block - 1) / block : 1;
+  const int nchunk = pick_nchunk(ctx, batch, upper, ctx->target_workgroups, row_blocks, part.rows, kPackedTile, rows_upper <= kSparseRows,
+                                 topk > 0 ? union_pages(rows_upper, topk) : upper);
+  const AttnInputs in{q, active_idx, active_count, sel_pages, sel_count, cap};
+  hipError_t e;
+  {
+    StageTimer timer(ctx, st, LOSA_STAGE_ATTN);
+    e = launch_packed_attn(st, ctx->cfg.dtype, kv, ctx->sh, batch, in, pk, nchunk, rows_upper, known, part);
+  }
+  if (e != hipSuccess) return hip_fail(ctx, "packed attention launch", e);
+  StageTimer timer(ctx, st, LOSA_STAGE_MERGE);
+  e = launch_attn_merge(st, kv, ctx->sh, batch, in, true, nchunk, part, o_p, lse_p, known ? rows_upper : 0, kPackedTile, kPackedTile);
+  if (e != hipSuccess) return hip_fail(ctx, "attn_merge launch", e);
+  return LOSA_OK;
+}
+
+losa_status check_attn_lists(losa_ctx* ctx, const char* call, const void* q, const int32_t* active_idx, const int32_t* active_count,
+                             const int32_t* sel_pages, const int32_t* sel_count, int32_t cap, const void* o_p, const float* lse_p) {
+  if (!q || !o_p || !lse_p) return fail(ctx, LOSA_ERR_INVALID_ARG, "%s: NULL pointer", call);
+  if ((active_idx == nullptr) != (active_count == nullptr))
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "active_idx and active_count must both be given or both be NULL");
+  if ((sel_pages == nullptr) != (sel_count == nullptr))
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "sel_pages and sel_count must both be given or both be NULL");
+  if (sel_pages && cap < 1) return fail(ctx, LOSA_ERR_INVALID_ARG, "cap must be >= 1");
+  return LOSA_OK;
+}
+
+// A denoising step over a cache of T (pk: NULL) or in 4 bits; the page table has been checked.
+losa_status step_impl(losa_ctx* ctx, hipStream_t st, const KvView& view, const PackedView* pk, int batch, int msp, int32_t step_index,
+                      const void* h_cur, const void* h_prev, const void* q, losa_select_mode mode, float param, int32_t topk_pages,
+                      void* o_p, float* lse_p, uint8_t* mask, int32_t* sel_count) {
+  if (step_index < 0) return fail(ctx, LOSA_ERR_INVALID_ARG, "step_index is negative");
+  if (!q || !o_p || !lse_p) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_step: NULL pointer");
+  if (step_index == 0)
+    return pk ? packed_attn_impl(ctx, st, view, *pk, batch, msp, q, nullptr, nullptr, nullptr, nullptr, 0, 0, (float*)o_p, lse_p)
+              : sparse_attn_impl(ctx, st, view, batch, msp, q, nullptr, nullptr, nullptr, nullptr, 0, 0, (float*)o_p, lse_p);
+  if (!h_cur || !h_prev) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_step: h_cur / h_prev are NULL");
+  if (topk_pages < 1 || topk_pages > ctx->cfg.max_topk_pages)
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "topk_pages %d outside 1..max_topk_pages (%d)", topk_pages,
+                ctx->cfg.max_topk_pages);
+  uint8_t* mk = mask ? mask : ctx->mask;
+  int32_t* sc = sel_count ? sel_count : ctx->sel_count;
+  // Where the scoring kernel can rank the locality scores itself, the locality launch only
+  // computes them: its end-of-kernel hand-over (store, wait, ticket, reload, rank) drops out
+  // of the step's chain of dependent launches.
+  InKernelRanking ranking{ctx->delta, (int)mode, 0, 0.f, mk, ctx->active_idx, ctx->active_count};
+  const bool rank_in_scores = ctx->rank_in_scores && ctx->cfg.dtype == LOSA_BF16 && ctx->sh.B <= 256;
+  losa_status s = parse_select(ctx, (int)mode, param, &ranking.n, &ranking.tau);
+  if (s != LOSA_OK) return s;
+  const int cap = ctx->sh.max_pages;
+  const bool bf16 = ctx->cfg.dtype == LOSA_BF16;
+  // the host knows |A| in the top-n modes, so selection and attention can be shaped for n*G rows
+  const bool counted = mode == LOSA_SEL_TOPK || mode == LOSA_SEL_FRACTION;
+  const int rows_upper = counted ? select_count(ctx, (int)mode, param) * ctx->sh.G : 0;
+  // The attention workgroups build the union of the per-row picks themselves, and the selection kernel ends with ORing
+  // them into the head's bitmap (for more than 64 rows only the shared-stage kernel does).  With a count only
+  // the device knows the attention launches take their row-tile counts from the device.
+  const bool few_only = (counted ? rows_upper : ctx->sh.rows_max) <= kSparseRows;
+  const bool union_in_attn = bf16 && !pk && ctx->union_in_attention && (!counted || rows_upper >= 1) && (few_only || ctx->shared_tiles);
+  const int union_upper = counted ? rows_upper : ctx->sh.rows_max;
+  const UnionInKernel uni{ctx->union_bits, ctx->entries, ctx->q_act, sc, union_words(ctx->sh.max_pages, ctx->sh.rows_max),
+                          union_copy_words(msp), union_copies(union_copy_words(msp), union_upper)};
+  // Short prefixes: scoring and selection in one launch.  (Not while stages are timed, which takes a launch for each, nor where
+  // the caller shapes the grid of either.)
+  const bool picked = rank_in_scores && union_in_attn && !ctx->profiling && ctx->select_round == 0 && ctx->score_round == kScoreRound &&
+                      pick_pages_serves(ctx->sh, batch, msp, union_upper, counted);
+  if (rank_in_scores) {
+    const bool takes_hidden = picked && pick_takes_hidden(ctx->sh);
+    if (!takes_hidden) {
+      StageTimer timer(ctx, st, LOSA_STAGE_LOCALITY);
+      hipError_t e = launch_locality_delta(st, ctx->cfg.dtype, h_cur, h_prev, batch, ctx->sh.B, ctx->sh.H, ctx->delta);
+      if (e != hipSuccess) return hip_fail(ctx, "locality_delta launch", e);
+    }
+    if (picked) {
+      hipError_t e = launch_pick_pages(st, view, ctx->sh, batch, msp, q, takes_hidden ? h_cur : nullptr, takes_hidden ? h_prev : nullptr,
+                                       union_upper, topk_pages, ctx->tickets, sc, ctx->entries, ctx->q_act, ranking, ctx->union_bits);
+      if (e != hipSuccess) return hip_fail(ctx, "pick_pages launch", e);
+    }
+  } else {
+    s = select_active_impl(ctx, st, batch, h_cur, h_prev, (int)mode, param, ctx->delta, mk, ctx->active_idx,
+                           ctx->active_count);
+    if (s != LOSA_OK) return s;
+  }
+  if (!picked)
+    s = score_pages_impl(ctx, st, view, batch, msp, q, ctx->active_idx, ctx->active_count, topk_pages, nullptr,
+                         ctx->sel_pages, sc, cap, rows_upper, rank_in_scores ? &ranking : nullptr,
+                         union_in_attn ? ctx->union_bits : nullptr);
+  if (s != LOSA_OK) return s;
+  if (pk)
+    return packed_attn_impl(ctx, st, view, *pk, batch, msp, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc, cap, rows_upper,
+                            (float*)o_p, lse_p, topk_pages);
+  return sparse_attn_impl(ctx, st, view, batch, msp, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc,
+                          cap, rows_upper, (float*)o_p, lse_p, union_in_attn ? &uni : nullptr, topk_pages);
 }
 
 }  // namespace
@@ -702,13 +861,8 @@ losa_status losa_sparse_attn(losa_ctx* ctx, void* stream, const losa_kv* kv, con
   if (!ctx) return LOSA_ERR_INVALID_ARG;
   int msp;
   losa_status s = check_kv(ctx, kv, false, &msp);
+  if (s == LOSA_OK) s = check_attn_lists(ctx, "losa_sparse_attn", q, active_idx, active_count, sel_pages, sel_count, cap, o_p, lse_p);
   if (s != LOSA_OK) return s;
-  if (!q || !o_p || !lse_p) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_sparse_attn: NULL pointer");
-  if ((active_idx == nullptr) != (active_count == nullptr))
-    return fail(ctx, LOSA_ERR_INVALID_ARG, "active_idx and active_count must both be given or both be NULL");
-  if ((sel_pages == nullptr) != (sel_count == nullptr))
-    return fail(ctx, LOSA_ERR_INVALID_ARG, "sel_pages and sel_count must both be given or both be NULL");
-  if (sel_pages && cap < 1) return fail(ctx, LOSA_ERR_INVALID_ARG, "cap must be >= 1");
   return sparse_attn_impl(ctx, as_stream(stream), view_of(kv, msp), kv->batch, msp, q, active_idx, active_count, sel_pages,
                           sel_count, cap, /*rows_upper=*/0, (float*)o_p, lse_p);
 }
@@ -732,70 +886,115 @@ losa_status losa_step(losa_ctx* ctx, void* stream, const losa_kv* kv, int32_t st
                       void* o_p, float* lse_p, uint8_t* mask, int32_t* sel_count) {
   if (!ctx) return LOSA_ERR_INVALID_ARG;
   int msp;
-  const bool dense = step_index == 0;
-  losa_status s = check_kv(ctx, kv, !dense, &msp);
+  const losa_status s = check_kv(ctx, kv, step_index != 0, &msp);
   if (s != LOSA_OK) return s;
-  if (step_index < 0) return fail(ctx, LOSA_ERR_INVALID_ARG, "step_index is negative");
-  if (!q || !o_p || !lse_p) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_step: NULL pointer");
-  hipStream_t st = as_stream(stream);
-  const KvView view = view_of(kv, msp);
-  if (dense)
-    return sparse_attn_impl(ctx, st, view, kv->batch, msp, q, nullptr, nullptr, nullptr, nullptr, 0, 0,
-                            (float*)o_p, lse_p);
-  if (!h_cur || !h_prev) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_step: h_cur / h_prev are NULL");
-  if (topk_pages < 1 || topk_pages > ctx->cfg.max_topk_pages)
-    return fail(ctx, LOSA_ERR_INVALID_ARG, "topk_pages %d outside 1..max_topk_pages (%d)", topk_pages,
-                ctx->cfg.max_topk_pages);
-  uint8_t* mk = mask ? mask : ctx->mask;
-  int32_t* sc = sel_count ? sel_count : ctx->sel_count;
-  // Where the scoring kernel can rank the locality scores itself, the locality launch only
-  // computes them: its end-of-kernel hand-over (store, wait, ticket, reload, rank) drops out
-  // of the step's chain of dependent launches.
-  InKernelRanking ranking{ctx->delta, (int)mode, 0, 0.f, mk, ctx->active_idx, ctx->active_count};
-  const bool rank_in_scores = ctx->rank_in_scores && ctx->cfg.dtype == LOSA_BF16 && ctx->sh.B <= 256;
-  s = parse_select(ctx, (int)mode, param, &ranking.n, &ranking.tau);
+  return step_impl(ctx, as_stream(stream), view_of(kv, msp), nullptr, kv->batch, msp, step_index, h_cur, h_prev, q, mode, param, topk_pages,
+                   o_p, lse_p, mask, sel_count);
+}
+
+losa_status losa_step_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, int32_t step_index, const void* h_cur,
+                             const void* h_prev, const void* q, losa_select_mode mode, float param, int32_t topk_pages,
+                             void* o_p, float* lse_p, uint8_t* mask, int32_t* sel_count) {
+  if (!ctx) return LOSA_ERR_INVALID_ARG;
+  int msp;
+  KvView view;
+  PackedView pk;
+  const losa_status s = check_packed(ctx, kv, step_index != 0, &msp, &view, &pk);
   if (s != LOSA_OK) return s;
-  const int cap = ctx->sh.max_pages;
-  const bool bf16 = ctx->cfg.dtype == LOSA_BF16;
-  // the host knows |A| in the top-n modes, so selection and attention can be shaped for n*G rows
-  const bool counted = mode == LOSA_SEL_TOPK || mode == LOSA_SEL_FRACTION;
-  const int rows_upper = counted ? select_count(ctx, (int)mode, param) * ctx->sh.G : 0;
-  // The attention workgroups build the union of the per-row picks themselves, and the selection kernel ends with ORing
-  // them into the head's bitmap (for more than 64 rows only the shared-stage kernel does).  With a count only
-  // the device knows the attention launches take their row-tile counts from the device.
-  const bool few_only = (counted ? rows_upper : ctx->sh.rows_max) <= kSparseRows;
-  const bool union_in_attn = bf16 && ctx->union_in_attention && (!counted || rows_upper >= 1) && (few_only || ctx->shared_tiles);
-  const int union_upper = counted ? rows_upper : ctx->sh.rows_max;
-  const UnionInKernel uni{ctx->union_bits, ctx->entries, ctx->q_act, sc, union_words(ctx->sh.max_pages, ctx->sh.rows_max),
-                          union_copy_words(msp), union_copies(union_copy_words(msp), union_upper)};
-  // Short prefixes: scoring and selection in one launch.  (Not while stages are timed, which takes a launch for each, nor where
-  // the caller shapes the grid of either.)
-  const bool picked = rank_in_scores && union_in_attn && !ctx->profiling && ctx->select_round == 0 && ctx->score_round == kScoreRound &&
-                      pick_pages_serves(ctx->sh, kv->batch, msp, union_upper, counted);
-  if (rank_in_scores) {
-    const bool takes_hidden = picked && pick_takes_hidden(ctx->sh);
-    if (!takes_hidden) {
-      StageTimer timer(ctx, st, LOSA_STAGE_LOCALITY);
-      hipError_t e = launch_locality_delta(st, ctx->cfg.dtype, h_cur, h_prev, kv->batch, ctx->sh.B, ctx->sh.H, ctx->delta);
-      if (e != hipSuccess) return hip_fail(ctx, "locality_delta launch", e);
-    }
-    if (picked) {
-      hipError_t e = launch_pick_pages(st, view, ctx->sh, kv->batch, msp, q, takes_hidden ? h_cur : nullptr, takes_hidden ? h_prev : nullptr,
-                                       union_upper, topk_pages, ctx->tickets, sc, ctx->entries, ctx->q_act, ranking, ctx->union_bits);
-      if (e != hipSuccess) return hip_fail(ctx, "pick_pages launch", e);
-    }
-  } else {
-    s = select_active_impl(ctx, st, kv->batch, h_cur, h_prev, (int)mode, param, ctx->delta, mk, ctx->active_idx,
-                           ctx->active_count);
-    if (s != LOSA_OK) return s;
-  }
-  if (!picked)
-    s = score_pages_impl(ctx, st, view, kv->batch, msp, q, ctx->active_idx, ctx->active_count, topk_pages, nullptr,
-                         ctx->sel_pages, sc, cap, rows_upper, rank_in_scores ? &ranking : nullptr,
-                         union_in_attn ? ctx->union_bits : nullptr);
+  return step_impl(ctx, as_stream(stream), view, &pk, kv->batch, msp, step_index, h_cur, h_prev, q, mode, param, topk_pages, o_p, lse_p,
+                   mask, sel_count);
+}
+
+losa_status losa_sparse_attn_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, const void* q, const int32_t* active_idx,
+                                    const int32_t* active_count, const int32_t* sel_pages, const int32_t* sel_count,
+                                    int32_t cap, void* o_p, float* lse_p) {
+  if (!ctx) return LOSA_ERR_INVALID_ARG;
+  int msp;
+  KvView view;
+  PackedView pk;
+  losa_status s = check_packed(ctx, kv, false, &msp, &view, &pk);
+  if (s == LOSA_OK) s = check_attn_lists(ctx, "losa_sparse_attn_packed", q, active_idx, active_count, sel_pages, sel_count, cap, o_p, lse_p);
   if (s != LOSA_OK) return s;
-  return sparse_attn_impl(ctx, st, view, kv->batch, msp, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc,
-                          cap, rows_upper, (float*)o_p, lse_p, union_in_attn ? &uni : nullptr, topk_pages);
+  return packed_attn_impl(ctx, as_stream(stream), view, pk, kv->batch, msp, q, active_idx, active_count, sel_pages, sel_count, cap,
+                          /*rows_upper=*/0, (float*)o_p, lse_p);
+}
+
+losa_status losa_rotate(losa_ctx* ctx, void* stream, const losa_rotation* rotation, const int32_t* positions, int32_t tokens,
+                        const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                        const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride) {
+  if (!ctx) return LOSA_ERR_INVALID_ARG;
+  if (!rotation) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_rotate: rotation is NULL");
+  Rotation rot;
+  const losa_status s = check_rotation(ctx, rotation, &rot);
+  if (s != LOSA_OK) return s;
+  if (tokens < 0) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_rotate: tokens is negative");
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr))
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_rotate: an input and its output must both be given or both be NULL");
+  if (tokens == 0 || (!q && !k)) return LOSA_OK;
+  if (!positions) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_rotate: positions is NULL");
+  const Shape& sh = ctx->sh;
+  const long qs = row_stride(ctx, q_stride, sh.Hq), qo = row_stride(ctx, q_out_stride, sh.Hq);
+  const long ks = row_stride(ctx, k_stride, sh.Hkv), ko = row_stride(ctx, k_out_stride, sh.Hkv);
+  if (unaligned(q) || unaligned(q_out) || unaligned(k) || unaligned(k_out) || (q && (!qs || !qo)) || (k && (!ks || !ko)))
+    return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_rotate: rows overlap or are not 16-byte aligned");
+  StageTimer timer(ctx, as_stream(stream), LOSA_STAGE_BLOCK);
+  const hipError_t e = launch_rotate(as_stream(stream), ctx->cfg.dtype, sh.d, rot, positions, tokens, q, qs, q_out, qo, sh.Hq, k, ks, k_out, ko, sh.Hkv);
+  if (e != hipSuccess) return hip_fail(ctx, "rotate launch", e);
+  return LOSA_OK;
+}
+
+losa_status losa_append_kv(losa_ctx* ctx, void* stream, const losa_kv* kv, const losa_new_tokens* fresh, const losa_rotation* rotation) {
+  if (!ctx) return LOSA_ERR_INVALID_ARG;
+  int msp, max_new;
+  NewTokens in;
+  Rotation rot;
+  losa_status s = check_kv(ctx, kv, false, &msp);
+  if (s == LOSA_OK && (unaligned(kv->k_pages) || unaligned(kv->v_pages) || unaligned(kv->meta)))
+    s = fail(ctx, LOSA_ERR_INVALID_ARG, "kv has a pool that is not 16-byte aligned");
+  if (s == LOSA_OK) s = check_new(ctx, fresh, &in, &max_new);
+  if (s == LOSA_OK) s = check_rotation(ctx, rotation, &rot);
+  if (s != LOSA_OK || max_new == 0) return s;
+  StageTimer timer(ctx, as_stream(stream), LOSA_STAGE_BOUNDS);
+  const hipError_t e = launch_append(as_stream(stream), ctx->cfg.dtype, view_of(kv, msp), ctx->sh, kv->batch, max_new, in, rot);
+  if (e != hipSuccess) return hip_fail(ctx, "append launch", e);
+  return LOSA_OK;
+}
+
+losa_status losa_append_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, const losa_new_tokens* fresh,
+                               const losa_rotation* rotation) {
+  if (!ctx) return LOSA_ERR_INVALID_ARG;
+  int msp, max_new;
+  KvView view;
+  PackedView pk;
+  NewTokens in;
+  Rotation rot;
+  losa_status s = check_packed(ctx, kv, false, &msp, &view, &pk);
+  if (s == LOSA_OK) s = check_new(ctx, fresh, &in, &max_new);
+  if (s == LOSA_OK) s = check_rotation(ctx, rotation, &rot);
+  if (s != LOSA_OK || max_new == 0) return s;
+  StageTimer timer(ctx, as_stream(stream), LOSA_STAGE_BOUNDS);
+  const hipError_t e = launch_append_packed(as_stream(stream), ctx->cfg.dtype, view, ctx->sh, kv->batch, max_new, in, rot, pk);
+  if (e != hipSuccess) return hip_fail(ctx, "append_packed launch", e);
+  return LOSA_OK;
+}
+
+losa_status losa_read_packed(losa_ctx* ctx, void* stream, const losa_packed_kv* kv, const int32_t* tok_indptr, int32_t num_tokens,
+                             int32_t max_tokens, void* k_out, void* v_out) {
+  if (!ctx) return LOSA_ERR_INVALID_ARG;
+  int msp;
+  KvView view;
+  PackedView pk;
+  const losa_status s = check_packed(ctx, kv, false, &msp, &view, &pk);
+  if (s != LOSA_OK) return s;
+  if (num_tokens < 0 || max_tokens < 0) return fail(ctx, LOSA_ERR_INVALID_ARG, "num_tokens and max_tokens must be >= 0");
+  if (num_tokens == 0 || (!k_out && !v_out)) return LOSA_OK;
+  if (!tok_indptr) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_read_packed: tok_indptr is NULL");
+  if (unaligned(k_out) || unaligned(v_out)) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_read_packed: an output is not 16-byte aligned");
+  const int most = max_tokens > 0 && max_tokens < num_tokens ? max_tokens : num_tokens;
+  StageTimer timer(ctx, as_stream(stream), LOSA_STAGE_BOUNDS);
+  const hipError_t e = launch_read_packed(as_stream(stream), ctx->cfg.dtype, view, ctx->sh, kv->batch, most, tok_indptr, num_tokens, pk, k_out, v_out);
+  if (e != hipSuccess) return hip_fail(ctx, "read_packed launch", e);
+  return LOSA_OK;
 }
 
 }  // extern "C"

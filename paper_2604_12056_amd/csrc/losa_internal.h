@@ -220,6 +220,42 @@ hipError_t launch_attn_rows(hipStream_t st, const KvView& kv, const Shape& sh, i
 hipError_t launch_attn_merge(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in,
                              bool bf16, int nchunk, const Partials& part, float* o_p, float* lse_p, int rows_hint, int few_tile, int many_tile);
 
+// ---- append_kv.hip
+struct NewTokens {
+  const void* k;              // T [num_tokens, Hkv, d], rows k_stride elements apart
+  const void* v;
+  long k_stride, v_stride;
+  const int32_t* indptr;      // [batch + 1]
+  const int32_t* positions;   // [num_tokens], or NULL: a token's place in its sequence
+  int num_tokens;
+};
+struct Rotation {
+  const float* table;         // [max_positions, rotary]; NULL: nothing is turned
+  int max_positions, rotary, pairs;
+};
+hipError_t launch_rotate(hipStream_t st, int dtype, int d, const Rotation& rot, const int32_t* positions, int tokens, const void* q,
+                         long q_stride, void* q_out, long q_out_stride, int q_heads, const void* k, long k_stride, void* k_out,
+                         long k_out_stride, int k_heads);
+hipError_t launch_append(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_new, const NewTokens& in,
+                         const Rotation& rot);
+
+// ---- packed_kv.hip and packed_attn.hip: the 4-bit cache (packed_format.h)
+struct PackedView {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* scales;
+};
+hipError_t launch_append_packed(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_new, const NewTokens& in,
+                                const Rotation& rot, const PackedView& out);
+hipError_t launch_read_packed(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_tokens, const int32_t* indptr,
+                              int num_tokens, const PackedView& in, void* k_out, void* v_out);
+// Tiles of 32 tokens are dealt round-robin to `nchunk` work items; partials in rows, references in log2 units.
+// rows: an upper bound on the query rows of a KV head; rows_known: the number itself.
+constexpr int kPackedTile = 32;
+inline int packed_block_rows(int dtype) { return dtype == LOSA_BF16 ? 64 : 32; }   // query rows of a workgroup
+hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
+                              int nchunk, int rows, bool rows_known, const Partials& part);
+
 // ---- block_merge.hip
 hipError_t launch_block_merge(hipStream_t st, int dtype, const Shape& sh, int batch, const void* q, const void* k_b,
                               const void* v_b, const float* o_p, const float* lse_p, float* out, float* o_b,
