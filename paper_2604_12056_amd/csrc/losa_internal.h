@@ -252,7 +252,7 @@ hipError_t launch_read_packed(hipStream_t st, int dtype, const KvView& kv, const
 // Tiles of 32 tokens are dealt round-robin to `nchunk` work items; partials in rows, references in log2 units.
 // rows: an upper bound on the query rows of a KV head; rows_known: the number itself.
 constexpr int kPackedTile = 32;
-inline int packed_block_rows(int dtype) { return dtype == LOSA_BF16 ? 64 : 32; }   // query rows of a workgroup
+inline int packed_block_rows(int dtype) { return dtype == LOSA_BF16 ? 256 : 32; }   // query rows of a workgroup, at most
 hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
                               int nchunk, int rows, bool rows_known, const Partials& part);
 

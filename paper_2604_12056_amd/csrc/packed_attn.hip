@@ -57,9 +57,59 @@ __device__ __forceinline__ void load_dwords(const uint8_t* p, uint32_t (&w)[N]) 
   }
 }
 
+// Scale bytes of four consecutive tokens' values: a dword per token, a byte per group.
+template <int J>
+__device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t (&w)[4]) {
+  if constexpr (J == 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
+    w[2] = x.z;
+    w[3] = x.w;
+  } else {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x & 0xFFFFu;
+    w[1] = x.x >> 16;
+    w[2] = x.y & 0xFFFFu;
+    w[3] = x.y >> 16;
+  }
+}
+
+// Group g's codes of four tokens under their scales: the halves of channel tiles 2 g (low codes) and 2 g + 1, tokens side by side.
+__device__ __forceinline__ void value_operands(uint32_t codes, const uint32_t (&scales)[4], int g, uint2& lo, uint2& hi) {
+  float f[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = power_of((scales[e] >> (8 * g)) & 0xFFu);
+  const uint32_t n0 = codes_to_f16<0>(codes, f[0]), n1 = codes_to_f16<1>(codes, f[1]);
+  const uint32_t n2 = codes_to_f16<2>(codes, f[2]), n3 = codes_to_f16<3>(codes, f[3]);
+  lo.x = __builtin_amdgcn_perm(n1, n0, 0x05040100u);
+  lo.y = __builtin_amdgcn_perm(n3, n2, 0x05040100u);
+  hi.x = __builtin_amdgcn_perm(n1, n0, 0x07060302u);
+  hi.y = __builtin_amdgcn_perm(n3, n2, 0x07060302u);
+}
+
+// Numerators of a lane's four tokens of two subtiles as pairs of halves; returns their sum.
+__device__ __forceinline__ float numerators(const f32x4_t& a, const f32x4_t& b, float scale_log2e, float neg_m, f16x8_t& p_hi, f16x8_t& p_lo) {
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const f32x4_t& s = e < 4 ? a : b;
+    const f32x2_t p = {__builtin_amdgcn_exp2f(fmaf(s[e & 3], scale_log2e, neg_m)), __builtin_amdgcn_exp2f(fmaf(s[(e & 3) + 1], scale_log2e, neg_m))};
+    sum += p[0] + p[1];
+    const f16x2_t hi = __builtin_convertvector(p, f16x2_t);
+    const f32x2_t rest = {p[0] - (float)hi[0], p[1] - (float)hi[1]};
+    const f16x2_t lo = __builtin_convertvector(rest, f16x2_t);
+    p_hi[e] = hi[0];
+    p_hi[e + 1] = hi[1];
+    p_lo[e] = lo[0];
+    p_lo[e + 1] = lo[1];
+  }
+  return sum;
+}
+
 // Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup does.
 template <int D, int GP, int R, int NQ, int NBUF>
-__device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int nchunk, int nrb,
+__device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int nchunk, int j,
                                                  int row0, const Partials& part, float scale_log2e, float* lds) {
   constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32;   // products per score, channel tiles, groups, dwords a lane reads of a subtile
   constexpr int CPL = D / 4;                                        // channels of a token that a lane has
@@ -67,7 +117,7 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
   constexpr int kTileBytes = GP * D / 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, qd = lane >> 4;
-  const int chunk = blockIdx.x, j = blockIdx.y / nrb, b = blockIdx.z, head = b * sh.Hkv + j;
+  const int chunk = blockIdx.x, b = blockIdx.z, head = b * sh.Hkv + j;
 
   const Sequence seq = sequence(kv, sh, b);
   const int M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
@@ -152,19 +202,7 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
       load_dwords<W>(pk.v + tile * kTileBytes + ((row / 4 + qd) * 16 + l16) * (J * 4), t.v[s]);
       const uint8_t* sc = pk.scales + tile * (2 * GP * J);
       t.ks[s] = sc[(row + l16) * J + qd * CPL / 32];
-      if constexpr (J == 4) {
-        const uint4 x = *reinterpret_cast<const uint4*>(sc + GP * J + (row + qd * 4) * J);
-        t.vs[s][0] = x.x;
-        t.vs[s][1] = x.y;
-        t.vs[s][2] = x.z;
-        t.vs[s][3] = x.w;
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(sc + GP * J + (row + qd * 4) * J);
-        t.vs[s][0] = x.x & 0xFFFFu;
-        t.vs[s][1] = x.x >> 16;
-        t.vs[s][2] = x.y & 0xFFFFu;
-        t.vs[s][3] = x.y >> 16;
-      }
+      load_scales<J>(sc + GP * J + (row + qd * 4) * J, t.vs[s]);
     }
   };
 
@@ -225,42 +263,13 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
     }
     f16x8_t p_hi[R], p_lo[R];
 #pragma unroll
-    for (int mt = 0; mt < R; ++mt) {
-      const float neg_m = -m_run[mt];
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const f32x2_t p = {__builtin_amdgcn_exp2f(fmaf(sc[mt][e >> 2][e & 3], scale_log2e, neg_m)),
-                           __builtin_amdgcn_exp2f(fmaf(sc[mt][e >> 2][(e & 3) + 1], scale_log2e, neg_m))};
-        sum += p[0] + p[1];
-        const f16x2_t hi = __builtin_convertvector(p, f16x2_t);
-        const f32x2_t rest = {p[0] - (float)hi[0], p[1] - (float)hi[1]};
-        const f16x2_t lo = __builtin_convertvector(rest, f16x2_t);
-        p_hi[mt][e] = hi[0];
-        p_hi[mt][e + 1] = hi[1];
-        p_lo[mt][e] = lo[0];
-        p_lo[mt][e + 1] = lo[1];
-      }
-      l_run[mt] += sum;
-    }
-    // values: group g's codes become the operands of channel tiles 2 g (low codes) and 2 g + 1
+    for (int mt = 0; mt < R; ++mt) l_run[mt] += numerators(sc[mt][0], sc[mt][1], scale_log2e, -m_run[mt], p_hi[mt], p_lo[mt]);
 #pragma unroll
     for (int g = 0; g < J; ++g) {
-      uint4 va, vb;
-      uint32_t* const a = &va.x;
-      uint32_t* const c = &vb.x;
+      uint2 lo[2], hi[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        float f[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = power_of((t.vs[s][e] >> (8 * g)) & 0xFFu);
-        const uint32_t n0 = codes_to_f16<0>(t.v[s][g], f[0]), n1 = codes_to_f16<1>(t.v[s][g], f[1]);
-        const uint32_t n2 = codes_to_f16<2>(t.v[s][g], f[2]), n3 = codes_to_f16<3>(t.v[s][g], f[3]);
-        a[2 * s] = __builtin_amdgcn_perm(n1, n0, 0x05040100u);
-        a[2 * s + 1] = __builtin_amdgcn_perm(n3, n2, 0x05040100u);
-        c[2 * s] = __builtin_amdgcn_perm(n1, n0, 0x07060302u);
-        c[2 * s + 1] = __builtin_amdgcn_perm(n3, n2, 0x07060302u);
-      }
+      for (int s = 0; s < 2; ++s) value_operands(t.v[s][g], t.vs[s], g, lo[s], hi[s]);
+      const uint4 va = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y), vb = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) {
         o[mt][2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, va), p_hi[mt], o[mt][2 * g], 0, 0, 0);
@@ -337,68 +346,309 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
   }
 }
 
+// ---- more than 32 query rows: the wavefronts of a workgroup have R*16 rows each and share the tiles.
+//
+// Two tiles of the workgroup's share are a stage of 64 tokens, four subtiles.  Every wavefront reads one subtile's codes (of keys and of values; with eight
+// wavefronts of one of them), converts them once for all rows and leaves them in LDS as the matrix core's operands, 16 bytes a lane, in lane
+// order.  Two LDS buffers and a barrier per stage; the codes of the next kAhead stages are on their way in registers (34 bytes a lane
+// and stage).
+template <int D>
+constexpr int kStageBytes = 64 * D * 2 * 2;   // keys, then values
+constexpr int kAhead = 2;
+
+template <int D, int GP, int R, int WAVES>
+__device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int nchunk, int j,
+                                                 int row_base, const Partials& part, float scale_log2e, char* lds) {
+  constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32, CPL = D / 4, PPT = 32 / GP, TPR = 64 / PPT;
+  constexpr int kTileBytes = GP * D / 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, qd = lane >> 4;
+  const int chunk = blockIdx.x, b = blockIdx.z, head = b * sh.Hkv + j;
+  const int row0 = row_base + wave * (R * 16);
+
+  const Sequence seq = sequence(kv, sh, b);
+  const int M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
+  const int U = min(in.list ? min(in.sel_count[head], in.cap) : seq.pages, sh.max_pages);
+  const int ntiles = (U + PPT - 1) / PPT;
+  if (row_base >= M || chunk >= ntiles) return;
+  const int mytiles = (ntiles - 1 - chunk) / nchunk + 1, stages = (mytiles + 1) / 2;
+
+  bf16x8_t qf[R][KS];
+#pragma unroll
+  for (int mt = 0; mt < R; ++mt) {
+    const int r = row0 + mt * 16 + l16, rr = min(r, sh.rows_max - 1), a = row_token(sh, rr);
+    const int tok = in.active_idx ? in.active_idx[(size_t)b * sh.B + a] : a;
+    const bool keep = r < M && (unsigned)tok < (unsigned)sh.B;
+    const bf16_t* row = (const bf16_t*)in.q + (((size_t)b * sh.B + (keep ? tok : 0)) * sh.Hq + j * sh.G + (rr - a * sh.G)) * D + qd * CPL;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      uint4 x = *reinterpret_cast<const uint4*>(row + ks * 8);
+      if (!keep) x = make_uint4(0u, 0u, 0u, 0u);
+      qf[mt][ks] = __builtin_bit_cast(bf16x8_t, x);
+    }
+  }
+
+  // pages of the share's next TPR tiles, one per lane
+  int pg_phys = 0, pg_valid = 0;
+  auto fetch_pages = [&](int n0) {
+    const int at = (chunk + (n0 + lane / PPT) * nchunk) * PPT + lane % PPT;
+    int logical = -1, phys = -1;
+    if (at < U) logical = in.list ? in.list[(size_t)head * in.cap + at] : at;
+    if ((unsigned)logical < (unsigned)seq.pages) phys = kv.page_indices[seq.base + logical];
+    const bool ok = (unsigned)phys < (unsigned)kv.num_pages;
+    pg_phys = ok ? phys : 0;
+    pg_valid = ok ? min(GP, seq.tokens - logical * GP) : 0;
+  };
+  // valid tokens of subtile s of stage i (of the TPR tiles at hand)
+  auto valid_of = [&](int i, int s) {
+    const int at = (2 * i + s / 2) * PPT;
+    return GP == 16 ? __builtin_amdgcn_readlane(pg_valid, (at + s % 2) & 63) : __builtin_amdgcn_readlane(pg_valid, at & 63) - 16 * (s % 2);
+  };
+
+  constexpr bool kBoth = WAVES == 4;
+  struct Raw {
+    uint32_t c[kBoth ? 2 * W : W], vs[4], ks;   // codes of keys and values, or of those that this wavefront brings
+  };
+  constexpr int kV = kBoth ? W : 0;
+  const bool has_keys = kBoth || wave < 4;
+  const int mysub = wave & 3;
+  auto load_stage = [&](Raw& x, int i) {   // (past the end: the pool's first page, as nothing depends on it)
+    const int at = ((2 * i + mysub / 2) * PPT + (GP == 16 ? mysub % 2 : 0)) & 63;
+    const size_t tile = (size_t)__builtin_amdgcn_readlane(pg_phys, at) * sh.Hkv + j;
+    const int row = GP == 16 ? 0 : 16 * (mysub % 2);
+    const uint8_t* sc = pk.scales + tile * (2 * GP * J);
+    const uint8_t* keys = pk.k + tile * kTileBytes + (row + l16) * (D / 2) + qd * (CPL / 2);
+    const uint8_t* values = pk.v + tile * kTileBytes + ((row / 4 + qd) * 16 + l16) * (J * 4);
+    uint32_t w[W];
+    load_dwords<W>(has_keys ? keys : values, w);
+#pragma unroll
+    for (int k = 0; k < W; ++k) x.c[k] = w[k];
+    if constexpr (kBoth) {
+      load_dwords<W>(values, w);
+#pragma unroll
+      for (int k = 0; k < W; ++k) x.c[W + k] = w[k];
+    }
+    x.ks = sc[(row + l16) * J + qd * CPL / 32];   // (with eight wavefronts each has one of the two in vain: no branch around a load)
+    load_scales<J>(sc + GP * J + (row + qd * 4) * J, x.vs);
+  };
+  auto convert_stage = [&](Raw& x, int i, char* buf) {
+    if (has_keys) {
+      const float scale = power_of(x.ks);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        *reinterpret_cast<uint4*>(buf + ((mysub * KS + ks) * 64 + lane) * 16) =
+            make_uint4(codes_to_bf16<0>(x.c[ks], scale), codes_to_bf16<1>(x.c[ks], scale), codes_to_bf16<2>(x.c[ks], scale), codes_to_bf16<3>(x.c[ks], scale));
+    }
+    if (kBoth || !has_keys) {
+      const int valid = valid_of(i, mysub);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.vs[e] = qd * 4 + e < valid ? x.vs[e] : 0u;   // (see the other form)
+      char* v = buf + 64 * D * 2 + ((mysub / 2) * NT * 64 + lane) * 16 + (mysub % 2) * 8;
+#pragma unroll
+      for (int g = 0; g < J; ++g) {
+        uint2 lo, hi;
+        value_operands(x.c[kV + g], x.vs, g, lo, hi);
+        *reinterpret_cast<uint2*>(v + (2 * g) * 1024) = lo;
+        *reinterpret_cast<uint2*>(v + (2 * g + 1) * 1024) = hi;
+      }
+    }
+  };
+
+  float m_run[R], l_run[R], up_thr[R];
+  const float inv_scale_log2e = 1.0f / scale_log2e;
+  f32x4_t o[R][NT];
+#pragma unroll
+  for (int mt = 0; mt < R; ++mt) {
+    m_run[mt] = kNegBig;
+    up_thr[mt] = -INFINITY;
+    l_run[mt] = 0.f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) o[mt][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  }
+  const bool has_rows = row0 < M;   // (the others convert only)
+
+  auto compute_stage = [&](int i, const char* buf, bool first) {
+    f32x4_t sc[R][4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+#pragma unroll
+      for (int mt = 0; mt < R; ++mt) sc[mt][s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(buf + ((s * KS + ks) * 64 + lane) * 16);
+#pragma unroll
+        for (int mt = 0; mt < R; ++mt) sc[mt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][ks], sc[mt][s], 0, 0, 0);
+      }
+    }
+    int nv[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) nv[s] = valid_of(i, s);
+    if (!(nv[0] >= 16 && nv[1] >= 16 && nv[2] >= 16 && nv[3] >= 16)) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int mt = 0; mt < R; ++mt) sc[mt][s][e] = qd * 4 + e < nv[s] ? sc[mt][s][e] : -INFINITY;
+    }
+    float tm[R];
+    bool any_up = false;
+#pragma unroll
+    for (int mt = 0; mt < R; ++mt) {
+      tm[mt] = sc[mt][0][0];
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tm[mt] = fmaxf(tm[mt], sc[mt][s][e]);
+      any_up |= tm[mt] > up_thr[mt];
+    }
+    if (__any(any_up)) {
+#pragma unroll
+      for (int mt = 0; mt < R; ++mt) {
+        const float cand = over_lane_groups_max(tm[mt]) * scale_log2e - kHeadroom;
+        const bool up = cand > m_run[mt] + kLag;
+        const float alpha = up ? __builtin_amdgcn_exp2f(m_run[mt] - cand) : 1.0f;
+        m_run[mt] = up ? cand : m_run[mt];
+        up_thr[mt] = (m_run[mt] + kHeadroom + kLag) * inv_scale_log2e;
+        l_run[mt] *= alpha;
+        if (!first) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) o[mt][nt] *= alpha;
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {   // a pair of subtiles at a time
+      f16x8_t p_hi[R], p_lo[R];
+#pragma unroll
+      for (int mt = 0; mt < R; ++mt) l_run[mt] += numerators(sc[mt][2 * h], sc[mt][2 * h + 1], scale_log2e, -m_run[mt], p_hi[mt], p_lo[mt]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const f16x8_t vf = *reinterpret_cast<const f16x8_t*>(buf + 64 * D * 2 + ((h * NT + nt) * 64 + lane) * 16);
+#pragma unroll
+        for (int mt = 0; mt < R; ++mt) o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_hi[mt], o[mt][nt], 0, 0, 0);
+#pragma unroll
+        for (int mt = 0; mt < R; ++mt) o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_lo[mt], o[mt][nt], 0, 0, 0);
+      }
+    }
+  };
+
+  constexpr int SPF = TPR / 2;   // stages per fetch of page entries
+  Raw raw[kAhead];
+  for (int n0 = 0; n0 < stages; n0 += SPF) {
+    const int ne = min(stages - n0, SPF);   // stages of this fetch, counted from its first
+    fetch_pages(2 * n0);
+    if (n0 > 0) __syncthreads();            // the buffers' last readers are done
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) load_stage(raw[k], k);
+    convert_stage(raw[0], 0, lds);
+    load_stage(raw[0], kAhead);
+    __syncthreads();
+    for (int i = 0; i < ne; i += 2) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (i + k >= ne) break;
+        // stage i + k is in buffer k, the next one goes to the other
+        if (i + k + 1 < ne) convert_stage(raw[(k + 1) % kAhead], i + k + 1, lds + (1 - k) * kStageBytes<D>);
+        load_stage(raw[(k + 1) % kAhead], i + k + 1 + kAhead);
+        if (has_rows) compute_stage(i + k, lds + k * kStageBytes<D>, n0 + i + k == 0);
+        __syncthreads();
+      }
+    }
+  }
+
+  const uint32_t item = (uint32_t)head * nchunk + chunk;
+#pragma unroll
+  for (int mt = 0; mt < R; ++mt) {
+    const float l = over_lane_groups_sum(l_run[mt]);
+    const int r = row0 + mt * 16 + l16;
+    if (r >= M) continue;
+    const uint32_t prow = item * part.rows + r;
+    if (qd == 0) {
+      part.m[prow] = m_run[mt];
+      part.l[prow] = l;
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + nt * 16 + qd * 4) = o[mt][nt];
+  }
+}
+
+// Up to 32 rows: the form whose wavefronts deal the tiles out.
+constexpr int kDealtRows = 32;
 template <int R, int D>
-constexpr size_t packed_lds_bytes() { return 4 * (R * (D / 16) * 256 + 2 * R * 16) * sizeof(float); }
+constexpr int packed_lds_bytes() { return 4 * (R * (D / 16) * 256 + 2 * R * 16) * (int)sizeof(float); }
 
 // Rows that the host knows: blocks of R row tiles.
 template <int D, int GP, int R, int NQ>
 __global__ __launch_bounds__(256) void packed_attn_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
                                                           float scale_log2e) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  packed_attn_body<D, GP, R, NQ, 3>(kv, sh, in, pk, nchunk, nrb, (int)(blockIdx.y % nrb) * (R * 16), part, scale_log2e, lds);
+  packed_attn_body<D, GP, R, NQ, 3>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (R * 16), part, scale_log2e, lds);
 }
-// Rows counted on the device: every block of MOST row tiles takes the form made for the rows it has.
-template <int D, int GP, int MOST, int NQ>
+// ... blocks of WAVES * R row tiles.
+template <int D, int GP, int R, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void packed_rows_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
+                                                                 float scale_log2e) {
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  packed_rows_body<D, GP, R, WAVES>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (WAVES * R * 16), part, scale_log2e,
+                                    reinterpret_cast<char*>(lds));
+}
+// Rows counted on the device: the form made for the rows a head has, block after block.  (Workgroups of their own for blocks that most
+// heads do not have would take turns with the others in the launch order, which leaves whole dies with nothing else.)
+template <int D, int GP, int NQ>
 __global__ __launch_bounds__(256) void packed_attn_counted_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
                                                                   float scale_log2e) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  const int row0 = (int)(blockIdx.y % nrb) * (MOST * 16), left = active_rows(in, kv, sh, blockIdx.z) - row0;
-  if (left <= 0) return;
-  if (left <= 16)
-    packed_attn_body<D, GP, 1, NQ, 3>(kv, sh, in, pk, nchunk, nrb, row0, part, scale_log2e, lds);
-  else if (left <= 32 || MOST == 2)
-    packed_attn_body<D, GP, 2, NQ, 3>(kv, sh, in, pk, nchunk, nrb, row0, part, scale_log2e, lds);
-  else if constexpr (MOST > 2) {
-    if (left <= 48)
-      packed_attn_body<D, GP, 3, NQ, 3>(kv, sh, in, pk, nchunk, nrb, row0, part, scale_log2e, lds);
-    else
-      packed_attn_body<D, GP, 4, NQ, 3>(kv, sh, in, pk, nchunk, nrb, row0, part, scale_log2e, lds);
+  const int M = min(active_rows(in, kv, sh, blockIdx.z), min(sh.rows_max, part.rows)), j = blockIdx.y;
+  if (M <= 16) {
+    packed_attn_body<D, GP, 1, NQ, 3>(kv, sh, in, pk, nchunk, j, 0, part, scale_log2e, lds);
+  } else if (M <= kDealtRows) {
+    packed_attn_body<D, GP, 2, NQ, 3>(kv, sh, in, pk, nchunk, j, 0, part, scale_log2e, lds);
+  } else {
+    constexpr int kRows = NQ == 1 ? 64 : 32;
+    for (int row0 = 0; row0 < M; row0 += kRows) {
+      if constexpr (NQ == 1)
+        packed_rows_body<D, GP, 1, 4>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, reinterpret_cast<char*>(lds));
+      else
+        packed_attn_body<D, GP, 2, NQ, 3>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
+      __syncthreads();   // the LDS is the next block's
+    }
   }
 }
 
-template <int D, int GP, int R, int NQ, bool COUNTED>
-static hipError_t launch_one(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk, int nchunk,
-                             int rows, const Partials& part) {
-  constexpr size_t lds_bytes = packed_lds_bytes<R, D>();
-  void (*kern)(KvView, Shape, AttnInputs, PackedView, int, int, Partials, float);
-  if constexpr (COUNTED)
-    kern = packed_attn_counted_kernel<D, GP, R, NQ>;
-  else
-    kern = packed_attn_kernel<D, GP, R, NQ>;
-  static bool attr_set = false;   // per instantiation
+typedef void (*PackedKernel)(KvView, Shape, AttnInputs, PackedView, int, int, Partials, float);
+
+// block_rows: query rows of a workgroup; 0: all of them, counted on the device
+template <int D, int GP>
+static hipError_t launch_one(PackedKernel kern, bool& attr_set, int waves, int lds_bytes, int block_rows, hipStream_t st, const KvView& kv, const Shape& sh,
+                             int batch, const AttnInputs& in, const PackedView& pk, int nchunk, int rows, const Partials& part) {
   if (lds_bytes > 48 * 1024 && !attr_set) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
     if (e != hipSuccess) return e;
     attr_set = true;
   }
-  const int nrb = (rows + R * 16 - 1) / (R * 16);
-  kern<<<dim3(nchunk, sh.Hkv * nrb, batch), 256, lds_bytes, st>>>(kv, sh, in, pk, nchunk, nrb, part, sh.sm_scale * 1.4426950408889634f);
+  const int nrb = block_rows ? (rows + block_rows - 1) / block_rows : 1;
+  kern<<<dim3(nchunk, sh.Hkv * nrb, batch), 64 * waves, lds_bytes, st>>>(kv, sh, in, pk, nchunk, nrb, part, sh.sm_scale * 1.4426950408889634f);
   return hipGetLastError();
 }
 
 template <int D, int GP>
 static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
                             int nchunk, int rows, bool known, const Partials& part) {
+  static bool attr_set[9];   // per kernel
+  auto go = [&](int which, PackedKernel kern, int waves, int lds_bytes, int block_rows) {
+    return launch_one<D, GP>(kern, attr_set[which], waves, lds_bytes, block_rows, st, kv, sh, batch, in, pk, nchunk, rows, part);
+  };
+  constexpr int kDealt1 = packed_lds_bytes<1, D>(), kDealt2 = packed_lds_bytes<2, D>(), kStaged = 2 * kStageBytes<D>;
   if (dtype != LOSA_BF16) {
-    if (rows <= 16) return launch_one<D, GP, 1, 3, false>(st, kv, sh, batch, in, pk, nchunk, rows, part);
-    return known ? launch_one<D, GP, 2, 3, false>(st, kv, sh, batch, in, pk, nchunk, rows, part)
-                 : launch_one<D, GP, 2, 3, true>(st, kv, sh, batch, in, pk, nchunk, rows, part);
+    if (rows <= 16) return go(0, packed_attn_kernel<D, GP, 1, 3>, 4, kDealt1, 16);
+    return known ? go(1, packed_attn_kernel<D, GP, 2, 3>, 4, kDealt2, 32) : go(2, packed_attn_counted_kernel<D, GP, 3>, 4, kDealt2, 0);
   }
-  if (rows <= 16) return launch_one<D, GP, 1, 1, false>(st, kv, sh, batch, in, pk, nchunk, rows, part);
-  if (!known) return launch_one<D, GP, 4, 1, true>(st, kv, sh, batch, in, pk, nchunk, rows, part);
-  if (rows <= 32) return launch_one<D, GP, 2, 1, false>(st, kv, sh, batch, in, pk, nchunk, rows, part);
-  if (rows <= 48) return launch_one<D, GP, 3, 1, false>(st, kv, sh, batch, in, pk, nchunk, rows, part);
-  return launch_one<D, GP, 4, 1, false>(st, kv, sh, batch, in, pk, nchunk, rows, part);
+  if (rows <= 16) return go(3, packed_attn_kernel<D, GP, 1, 1>, 4, kDealt1, 16);
+  if (!known) return go(4, packed_attn_counted_kernel<D, GP, 1>, 4, kStaged > kDealt2 ? kStaged : kDealt2, 0);
+  if (rows <= kDealtRows) return go(5, packed_attn_kernel<D, GP, 2, 1>, 4, kDealt2, 32);
+  if (rows <= 64) return go(6, packed_rows_kernel<D, GP, 1, 4>, 4, kStaged, 64);
+  return rows <= 128 ? go(7, packed_rows_kernel<D, GP, 1, 8>, 8, kStaged, 128) : go(8, packed_rows_kernel<D, GP, 2, 8>, 8, kStaged, 256);
 }
 
 hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
