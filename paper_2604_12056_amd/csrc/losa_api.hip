@@ -514,7 +514,7 @@ losa_status sparse_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, in
 // The same over a 4-bit cache.
 losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, const PackedView& pk, int batch, int max_seq_pages, const void* q,
                              const int32_t* active_idx, const int32_t* active_count, const int32_t* sel_pages, const int32_t* sel_count,
-                             int cap, int rows_upper, float* o_p, float* lse_p, int topk = 0) {
+                             int cap, int rows_upper, float* o_p, float* lse_p) {
   const int upper = sel_pages ? (cap < max_seq_pages ? cap : max_seq_pages) : max_seq_pages;
   if (!active_idx) rows_upper = ctx->sh.rows_max;
   const bool known = rows_upper >= 1 && rows_upper <= ctx->sh.rows_max;
@@ -523,8 +523,10 @@ losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, co
   part.rows = known ? std::min((rows_upper + 15) / 16 * 16, ctx->sh.rows_max) : ctx->sh.rows_max;
   // (a count that only the device knows is mostly that of a few active tokens: shares as for one block of rows)
   const int block = packed_block_rows(ctx->cfg.dtype), row_blocks = known ? (rows_upper + block - 1) / block : 1;
-  const int nchunk = pick_nchunk(ctx, batch, upper, ctx->target_workgroups, row_blocks, part.rows, kPackedTile, rows_upper <= kSparseRows,
-                                 topk > 0 ? union_pages(rows_upper, topk) : upper);
+  const long heads = (long)batch * ctx->sh.Hkv, tiles = ((long)upper * ctx->sh.g + kPackedTile - 1) / kPackedTile;
+  long want = std::min(ctx->target_workgroups / (heads * row_blocks), ctx->part_rows / (heads * part.rows));
+  want = std::min(want, ctx->shares_set ? tiles : (tiles + 7) / 8);   // (a tile for each wavefront)
+  const int nchunk = (int)std::max(want, 1L);
   const AttnInputs in{q, active_idx, active_count, sel_pages, sel_count, cap};
   hipError_t e;
   {
@@ -612,7 +614,7 @@ losa_status step_impl(losa_ctx* ctx, hipStream_t st, const KvView& view, const P
   if (s != LOSA_OK) return s;
   if (pk)
     return packed_attn_impl(ctx, st, view, *pk, batch, msp, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc, cap, rows_upper,
-                            (float*)o_p, lse_p, topk_pages);
+                            (float*)o_p, lse_p);
   return sparse_attn_impl(ctx, st, view, batch, msp, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc,
                           cap, rows_upper, (float*)o_p, lse_p, union_in_attn ? &uni : nullptr, topk_pages);
 }

@@ -18,6 +18,8 @@
 // range and what lo cannot hold is below 2^-25, 2^-32 of the largest p.
 #include <math.h>
 
+#include <algorithm>
+
 #include "losa_device.h"
 #include "losa_internal.h"
 #include "packed_format.h"
@@ -55,6 +57,11 @@ __device__ __forceinline__ void load_dwords(const uint8_t* p, uint32_t (&w)[N]) 
     w[0] = x[0];
     w[1] = x[1];
   }
+}
+
+__device__ __forceinline__ void load_floats8(const float* p, float (&x)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
 }
 
 // Scale bytes of four consecutive tokens' values: a dword per token, a byte per group.
@@ -107,55 +114,135 @@ __device__ __forceinline__ float numerators(const f32x4_t& a, const f32x4_t& b, 
   return sum;
 }
 
-// Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup does.
-template <int D, int GP, int R, int NQ, int NBUF>
+// Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup of up to 64 rows does.  Its WAVES wavefronts deal the share's tiles out, two
+// wavefronts to a SIMD, so that one's matrix products run beside the other's vector work.  That takes 256 registers a lane at most:
+//   a tile's codes have no second buffer: the next tile's keys are requested when this one's have been converted, its values after
+//     the last product (what is on its way per compute unit is still some 24 KiB);
+//   the query fragments are read from LDS for every tile where there are more than two row tiles (or float queries).
+// Four row tiles do not fit.  They are two sets of two (SETS): a wavefront of each set takes every tile, which reads its codes from
+// the cache the second time and converts them twice, 128 of some 240 vector instructions a tile.
+constexpr int kSlots = 4;   // LDS images of a wavefront's state (of a set): half of the wavefronts hand theirs over, twice; with two sets all have one
+template <int R, int D, int NQ, int SETS = 1>
+struct DealtLds {
+  static constexpr bool kQueries = R > 2 || NQ > 1;
+  static constexpr int kState = R * (D / 16) * 256 + 2 * R * 16;                    // floats: O as [row tile][channel tile][lane] vectors, references, sums
+  static constexpr int kQueryFloats = kQueries ? NQ * R * (D / 32) * 256 : 0;
+  static constexpr int kBytes = (kQueryFloats + SETS * kSlots * kState) * (int)sizeof(float);
+};
+template <int D, int GP, int R, int NQ, int SETS = 1>
 __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int nchunk, int j,
-                                                 int row0, const Partials& part, float scale_log2e, float* lds) {
+                                                 int row_base, const Partials& part, float scale_log2e, float* lds) {
+  constexpr int WAVES = 2 * kSlots / SETS;   // of a set
   constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32;   // products per score, channel tiles, groups, dwords a lane reads of a subtile
   constexpr int CPL = D / 4;                                        // channels of a token that a lane has
   constexpr int PPT = 32 / GP, TPR = 64 / PPT;                      // pages per tile, tiles per fetch of page entries
   constexpr int kTileBytes = GP * D / 2;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  typedef DealtLds<R, D, NQ, SETS> Lds;
+  static_assert(SETS == 1 || !Lds::kQueries, "the sets' queries are not the same");
+  constexpr bool kTight = D == 128 && Lds::kQueries;   // registers are short
+  const int lane = threadIdx.x & 63, in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_group % WAVES, set = in_group / WAVES;
   const int l16 = lane & 15, qd = lane >> 4;
-  const int chunk = blockIdx.x, b = blockIdx.z, head = b * sh.Hkv + j;
+  const int chunk = blockIdx.x, b = blockIdx.z, head = b * sh.Hkv + j, row0 = row_base + set * (R * 16);
 
   const Sequence seq = sequence(kv, sh, b);
   const int M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
   const int U = min(in.list ? min(in.sel_count[head], in.cap) : seq.pages, sh.max_pages);
   const int ntiles = (U + PPT - 1) / PPT;
-  if (row0 >= M || chunk >= ntiles) return;
+  if (row_base >= M || chunk >= ntiles) return;
   // tiles are dealt round-robin to the workgroups, and a workgroup's to its wavefronts
-  const int tfirst = chunk + nchunk * wave, tstep = nchunk * 4;
+  const int tfirst = chunk + nchunk * wave, tstep = nchunk * WAVES;
   const int ntw = tfirst < ntiles ? (ntiles - 1 - tfirst) / tstep + 1 : 0;
 
-  // ---- query rows, in the order the keys' channels are contracted in
-  bf16x8_t qf[R][NQ][KS];
+  // ---- pages of this wavefront's next TPR tiles, one per lane
+  int pg_phys = 0, pg_valid = 0;
+  auto fetch_pages = [&](int n0) {
+    const int at = (tfirst + (n0 + lane / PPT) * tstep) * PPT + lane % PPT;
+    int logical = -1, phys = -1;
+    if (at < U) logical = in.list ? in.list[(size_t)head * in.cap + at] : at;
+    if ((unsigned)logical < (unsigned)seq.pages) phys = kv.page_indices[seq.base + logical];
+    const bool ok = (unsigned)phys < (unsigned)kv.num_pages;
+    pg_phys = ok ? phys : 0;
+    pg_valid = ok ? min(GP, seq.tokens - logical * GP) : 0;
+  };
+  struct Keys {
+    uint32_t c[2][W], s[2];
+  } k;
+  struct Values {
+    uint32_t c[2][W], s[2][4];   // s: scales of the lane's four tokens, a byte per group
+  } v;
+  int nv[2] = {0, 0}, nv_next[2] = {0, 0};   // valid tokens of the two subtiles
+  // tile n (where there is none, the pool's first page: nothing is made of it)
+  auto page_of = [&](int n, int s) {
+    const int at = GP == 16 ? (2 * n + s) & 63 : n & 63;
+    return n < ntw ? __builtin_amdgcn_readlane(pg_phys, at) : 0;
+  };
+  auto load_keys = [&](int n) {
 #pragma unroll
-  for (int mt = 0; mt < R; ++mt) {
-    const int r = row0 + mt * 16 + l16, a = row_token(sh, min(r, sh.rows_max - 1));
+    for (int s = 0; s < 2; ++s) {
+      const size_t tile = (size_t)page_of(n, s) * sh.Hkv + j;
+      const int row = (GP == 16 ? 0 : 16 * s) + l16;
+      load_dwords<W>(pk.k + tile * kTileBytes + row * (D / 2) + qd * (CPL / 2), k.c[s]);
+      k.s[s] = pk.scales[tile * (2 * GP * J) + row * J + qd * CPL / 32];
+      nv_next[s] = __builtin_amdgcn_readlane(pg_valid, GP == 16 ? (2 * n + s) & 63 : n & 63) - (GP == 16 ? 0 : 16 * s);
+    }
+  };
+  auto load_values = [&](int n) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const size_t tile = (size_t)page_of(n, s) * sh.Hkv + j;
+      const int quad = (GP == 16 ? 0 : 4 * s) + qd;
+      load_dwords<W>(pk.v + tile * kTileBytes + (quad * 16 + l16) * (J * 4), v.c[s]);
+      load_scales<J>(pk.scales + tile * (2 * GP * J) + GP * J + quad * 4 * J, v.s[s]);
+    }
+  };
+  fetch_pages(0);
+  load_keys(0);
+  load_values(0);
+
+  // ---- query rows, in the order the keys' channels are contracted in: fragment (row tile, term, product)
+  bf16x8_t qf[Lds::kQueries ? 1 : R][NQ][KS];
+  auto query = [&](int mt, int ks, bf16x8_t (&term)[NQ]) {
+    const int r = row0 + mt * 16 + l16, rr = min(r, sh.rows_max - 1), a = row_token(sh, rr);
     const int tok = in.active_idx ? in.active_idx[(size_t)b * sh.B + a] : a;
     const bool keep = r < M && (unsigned)tok < (unsigned)sh.B;
-    const size_t at = (((size_t)b * sh.B + (keep ? tok : 0)) * sh.Hq + j * sh.G + (min(r, sh.rows_max - 1) - a * sh.G)) * D + qd * CPL;
+    const size_t at = (((size_t)b * sh.B + (keep ? tok : 0)) * sh.Hq + j * sh.G + (rr - a * sh.G)) * D + qd * CPL + ks * 8;
+    if constexpr (NQ == 1) {
+      uint4 x = *reinterpret_cast<const uint4*>((const bf16_t*)in.q + at);
+      if (!keep) x = make_uint4(0u, 0u, 0u, 0u);
+      term[0] = __builtin_bit_cast(bf16x8_t, x);
+    } else {
+      float x[8];
+      load_floats8((const float*)in.q + at, x);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      if constexpr (NQ == 1) {
-        uint4 x = *reinterpret_cast<const uint4*>((const bf16_t*)in.q + at + ks * 8);
-        if (!keep) x = make_uint4(0u, 0u, 0u, 0u);
-        qf[mt][0][ks] = __builtin_bit_cast(bf16x8_t, x);
-      } else {
-        const float4 x0 = *reinterpret_cast<const float4*>((const float*)in.q + at + ks * 8), x1 = *reinterpret_cast<const float4*>((const float*)in.q + at + ks * 8 + 4);
-        float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+      for (int n = 0; n < NQ; ++n)
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (!keep) x[e] = 0.f;
-            const __bf16 t = (__bf16)x[e];
-            qf[mt][n][ks][e] = t;
-            x[e] -= (float)t;
-          }
-      }
+        for (int e = 0; e < 8; ++e) {
+          if (!keep) x[e] = 0.f;
+          const __bf16 t = (__bf16)x[e];
+          term[n][e] = t;
+          x[e] -= (float)t;
+        }
     }
+  };
+  const bf16x8_t* const q_lds = reinterpret_cast<const bf16x8_t*>(lds);
+  if constexpr (Lds::kQueries) {
+    for (int f = wave; f < R * KS; f += WAVES) {
+      bf16x8_t term[NQ];
+      query(f / KS, f % KS, term);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) reinterpret_cast<bf16x8_t*>(lds)[(f * NQ + n) * 64 + lane] = term[n];
+    }
+    __syncthreads();
+  } else {
+#pragma unroll
+    for (int mt = 0; mt < R; ++mt)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8_t term[NQ];
+        query(mt, ks, term);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) qf[mt][n][ks] = term[n];
+      }
   }
 
   float m_run[R], l_run[R], up_thr[R];
@@ -170,69 +257,45 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
     for (int nt = 0; nt < NT; ++nt) o[mt][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   }
 
-  // ---- pages of this wavefront's next TPR tiles, one per lane
-  int pg_phys = 0, pg_valid = 0;
-  auto fetch_pages = [&](int n0) {
-    const int at = (tfirst + (n0 + lane / PPT) * tstep) * PPT + lane % PPT;
-    int logical = -1, phys = -1;
-    if (at < U) logical = in.list ? in.list[(size_t)head * in.cap + at] : at;
-    if ((unsigned)logical < (unsigned)seq.pages) phys = kv.page_indices[seq.base + logical];
-    const bool ok = (unsigned)phys < (unsigned)kv.num_pages;
-    pg_phys = ok ? phys : 0;
-    pg_valid = ok ? min(GP, seq.tokens - logical * GP) : 0;
-  };
-
-  struct Tile {
-    uint32_t k[2][W], v[2][W], vs[2][4];   // vs: scales of the lane's four tokens, a byte per group (64 channels: two tokens a dword)
-    uint32_t ks[2];
-    int nv[2];   // valid tokens of the two subtiles
-  };
-  // A tile that does not exist is read like one, from the pool's first page, so that the loads in flight are the same number always.
-  auto load_tile = [&](Tile& t, int n, int ne) {
-    const bool real = n < ne;
-    const int slot = (n * PPT) & 63;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int at = GP == 16 ? slot + s : slot;
-      const int phys = real ? __builtin_amdgcn_readlane(pg_phys, at) : 0, valid = real ? __builtin_amdgcn_readlane(pg_valid, at) : 0;
-      t.nv[s] = GP == 16 ? valid : valid - 16 * s;
-      const int row = GP == 16 ? 0 : 16 * s;
-      const size_t tile = (size_t)phys * sh.Hkv + j;
-      load_dwords<W>(pk.k + tile * kTileBytes + (row + l16) * (D / 2) + qd * (CPL / 2), t.k[s]);
-      load_dwords<W>(pk.v + tile * kTileBytes + ((row / 4 + qd) * 16 + l16) * (J * 4), t.v[s]);
-      const uint8_t* sc = pk.scales + tile * (2 * GP * J);
-      t.ks[s] = sc[(row + l16) * J + qd * CPL / 32];
-      load_scales<J>(sc + GP * J + (row + qd * 4) * J, t.vs[s]);
-    }
-  };
-
-  auto compute_tile = [&](Tile& t, bool first) {
-    // scores
+  for (int n = 0; n < ntw; ++n) {
+    nv[0] = nv_next[0];
+    nv[1] = nv_next[1];
+    if ((n + 1) % TPR == 0) fetch_pages(n + 1);   // (the entries are decoded behind the branch, so nothing waits where it joins)
+    // scores, a subtile at a time (the barriers keep what is read or converted ahead, and so the registers, to that)
     f32x4_t sc[R][2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const float ks_scale = power_of(t.ks[s]);
+      const float scale = power_of(k.s[s]);
+      bf16x8_t kf[KS];
 #pragma unroll
-      for (int mt = 0; mt < R; ++mt) sc[mt][s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      for (int ks = 0; ks < KS; ++ks)
+        kf[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(codes_to_bf16<0>(k.c[s][ks], scale), codes_to_bf16<1>(k.c[s][ks], scale),
+                                                         codes_to_bf16<2>(k.c[s][ks], scale), codes_to_bf16<3>(k.c[s][ks], scale)));
+      if (s == 1) load_keys(n + 1);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const uint4 kf = make_uint4(codes_to_bf16<0>(t.k[s][ks], ks_scale), codes_to_bf16<1>(t.k[s][ks], ks_scale),
-                                    codes_to_bf16<2>(t.k[s][ks], ks_scale), codes_to_bf16<3>(t.k[s][ks], ks_scale));
+      for (int mt = 0; mt < R; ++mt) {
+        sc[mt][s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int mt = 0; mt < R; ++mt)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-          for (int n = NQ - 1; n >= 0; --n)
-            sc[mt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf), qf[mt][n][ks], sc[mt][s], 0, 0, 0);
+          for (int t = NQ - 1; t >= 0; --t) {
+            bf16x8_t q;
+            if constexpr (Lds::kQueries)
+              q = q_lds[((mt * KS + ks) * NQ + t) * 64 + lane];
+            else
+              q = qf[mt][t][ks];
+            sc[mt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks], q, sc[mt][s], 0, 0, 0);
+          }
       }
+      if constexpr (kTight) __builtin_amdgcn_sched_barrier(0);
     }
-    const bool full = t.nv[0] >= 16 && t.nv[1] >= 16;
-    if (!full) {   // slots behind the sequence's end may hold anything
+    if (!(nv[0] >= 16 && nv[1] >= 16)) {   // slots behind the sequence's end may hold anything
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const bool there = qd * 4 + e < t.nv[s];
-          t.vs[s][e] = there ? t.vs[s][e] : 0u;   // (the smallest scale: nothing, in half precision)
+          const bool there = qd * 4 + e < nv[s];
+          v.s[s][e] = there ? v.s[s][e] : 0u;   // (the smallest scale: nothing, in half precision)
 #pragma unroll
           for (int mt = 0; mt < R; ++mt) sc[mt][s][e] = there ? sc[mt][s][e] : -INFINITY;
         }
@@ -255,7 +318,7 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
         m_run[mt] = up ? cand : m_run[mt];
         up_thr[mt] = (m_run[mt] + kHeadroom + kLag) * inv_scale_log2e;
         l_run[mt] *= alpha;
-        if (!first) {
+        if (n > 0) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) o[mt][nt] *= alpha;
         }
@@ -268,95 +331,101 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
     for (int g = 0; g < J; ++g) {
       uint2 lo[2], hi[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) value_operands(t.v[s][g], t.vs[s], g, lo[s], hi[s]);
-      const uint4 va = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y), vb = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
+      for (int s = 0; s < 2; ++s) value_operands(v.c[s][g], v.s[s], g, lo[s], hi[s]);
+      const f16x8_t va = __builtin_bit_cast(f16x8_t, make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y));
+      const f16x8_t vb = __builtin_bit_cast(f16x8_t, make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y));
+      if (g == J - 1) load_values(n + 1);
+      if constexpr (kTight) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) {
-        o[mt][2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, va), p_hi[mt], o[mt][2 * g], 0, 0, 0);
-        o[mt][2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, vb), p_hi[mt], o[mt][2 * g + 1], 0, 0, 0);
+        o[mt][2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, p_hi[mt], o[mt][2 * g], 0, 0, 0);
+        o[mt][2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, p_hi[mt], o[mt][2 * g + 1], 0, 0, 0);
       }
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) {
-        o[mt][2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, va), p_lo[mt], o[mt][2 * g], 0, 0, 0);
-        o[mt][2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, vb), p_lo[mt], o[mt][2 * g + 1], 0, 0, 0);
-      }
-    }
-  };
-
-  Tile tb[NBUF];
-  for (int nb = 0; nb < ntw; nb += TPR) {
-    const int ne = min(ntw, nb + TPR);
-    fetch_pages(nb);
-#pragma unroll
-    for (int k = 0; k < NBUF - 1; ++k) load_tile(tb[k], nb + k, ne);
-    for (int n = nb; n < ne; n += NBUF) {
-#pragma unroll
-      for (int k = 0; k < NBUF; ++k) {
-        load_tile(tb[(k + NBUF - 1) % NBUF], n + k + NBUF - 1, ne);
-        if (n + k < ne) compute_tile(tb[k], n + k == 0);
+        o[mt][2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, p_lo[mt], o[mt][2 * g], 0, 0, 0);
+        o[mt][2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, p_lo[mt], o[mt][2 * g + 1], 0, 0, 0);
       }
     }
   }
 
-  // ---- the four wavefronts' states become one partial: everybody's in LDS, then a quarter of the channels each, in a fixed order
-  constexpr int kSlot = R * NT * 64 * 4 + 2 * R * 16;   // O as [row tile][channel tile][lane] vectors, then references and sums
-  float* mine = lds + wave * kSlot;
+  // ---- the wavefronts' states become one partial, in a fixed order: the second half of them hands its states to the first through LDS, those hand theirs
+  // to everybody, and each wavefront makes some of the partial's vectors
 #pragma unroll
-  for (int mt = 0; mt < R; ++mt) {
-    const float l = over_lane_groups_sum(l_run[mt]);
-    if (qd == 0) {
-      mine[R * NT * 256 + mt * 16 + l16] = m_run[mt];
-      mine[R * NT * 256 + R * 16 + mt * 16 + l16] = l;
+  for (int mt = 0; mt < R; ++mt) l_run[mt] = over_lane_groups_sum(l_run[mt]);
+  float* const states = lds + Lds::kQueryFloats;
+  float* const slot = states + (SETS == 1 ? wave % kSlots : in_group) * Lds::kState;
+  auto publish = [&]() {
+#pragma unroll
+    for (int mt = 0; mt < R; ++mt) {
+      if (qd == 0) {
+        slot[R * NT * 256 + mt * 16 + l16] = m_run[mt];
+        slot[R * NT * 256 + R * 16 + mt * 16 + l16] = l_run[mt];
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4_t*>(slot + ((mt * NT + nt) * 64 + lane) * 4) = o[mt][nt];
     }
+  };
+  if constexpr (SETS == 1) {
+    if (wave >= kSlots) publish();
+    __syncthreads();
+    if (wave < kSlots) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4_t*>(mine + ((mt * NT + nt) * 64 + lane) * 4) = o[mt][nt];
+      for (int mt = 0; mt < R; ++mt) {
+        const float m = slot[R * NT * 256 + mt * 16 + l16], l = slot[R * NT * 256 + R * 16 + mt * 16 + l16];
+        const float m_all = fmaxf(m_run[mt], m), mine = __builtin_amdgcn_exp2f(m_run[mt] - m_all), theirs = __builtin_amdgcn_exp2f(m - m_all);
+        m_run[mt] = m_all;
+        l_run[mt] = fmaf(l_run[mt], mine, l * theirs);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) o[mt][nt] = o[mt][nt] * mine + *reinterpret_cast<const f32x4_t*>(slot + ((mt * NT + nt) * 64 + lane) * 4) * theirs;
+      }
+      publish();   // (where this wavefront alone has just read)
+    }
+  } else {
+    publish();
   }
   __syncthreads();
   const uint32_t item = (uint32_t)head * nchunk + chunk;
-#pragma unroll
-  for (int mt = 0; mt < R; ++mt) {
-    const int r = row0 + mt * 16 + l16;
+  for (int piece = in_group; piece < SETS * R * NT; piece += SETS * WAVES) {
+    const int of = piece / (R * NT), vec = piece % (R * NT), mt = vec / NT, nt = vec % NT, r = row_base + of * (R * 16) + mt * 16 + l16;
     if (r >= M) continue;
-    float m[4], l[4];
+    float m[kSlots], l[kSlots], m_all = kNegBig;
+    f32x4_t x[kSlots];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      m[w] = lds[w * kSlot + R * NT * 256 + mt * 16 + l16];
-      l[w] = lds[w * kSlot + R * NT * 256 + R * 16 + mt * 16 + l16];
+    for (int w = 0; w < kSlots; ++w) {
+      const float* from = states + (of * kSlots + w) * Lds::kState;
+      m[w] = from[R * NT * 256 + mt * 16 + l16];
+      l[w] = from[R * NT * 256 + R * 16 + mt * 16 + l16];
+      x[w] = *reinterpret_cast<const f32x4_t*>(from + (vec * 64 + lane) * 4);
+      m_all = fmaxf(m_all, m[w]);
     }
-    const float m_all = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-    float wgt[4], l_all = 0.f;
+    float l_all = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      wgt[w] = __builtin_amdgcn_exp2f(m[w] - m_all);
-      l_all = fmaf(l[w], wgt[w], l_all);
+    for (int w = 0; w < kSlots; ++w) {
+      const float wgt = __builtin_amdgcn_exp2f(m[w] - m_all);
+      l_all = fmaf(l[w], wgt, l_all);
+      acc += x[w] * wgt;
     }
     const uint32_t prow = item * part.rows + r;
-    if (wave == 0 && qd == 0) {
+    if (nt == 0 && qd == 0) {
       part.m[prow] = m_all;
       part.l[prow] = l_all;
     }
-#pragma unroll
-    for (int k = 0; k < NT / 4; ++k) {
-      const int nt = wave * (NT / 4) + k;
-      f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) acc += *reinterpret_cast<const f32x4_t*>(lds + w * kSlot + ((mt * NT + nt) * 64 + lane) * 4) * wgt[w];
-      *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + nt * 16 + qd * 4) = acc;
-    }
+    *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + nt * 16 + qd * 4) = acc;
   }
 }
 
-// ---- more than 32 query rows: the wavefronts of a workgroup have R*16 rows each and share the tiles.
+// ---- more than 64 query rows: the eight wavefronts of a workgroup have R*16 rows each and share the tiles.
 //
-// Two tiles of the workgroup's share are a stage of 64 tokens, four subtiles.  Every wavefront reads one subtile's codes (of keys and of values; with eight
-// wavefronts of one of them), converts them once for all rows and leaves them in LDS as the matrix core's operands, 16 bytes a lane, in lane
-// order.  Two LDS buffers and a barrier per stage; the codes of the next kAhead stages are on their way in registers (34 bytes a lane
-// and stage).
+// Two tiles of the workgroup's share are a stage of 64 tokens, four subtiles.  Every wavefront reads one subtile's codes, of keys or of values, converts
+// them once for all rows and leaves them in LDS as the matrix core's operands, 16 bytes a lane, in lane order.  Two LDS buffers and
+// a barrier per stage; the codes of the next kAhead stages are on their way in registers.
 template <int D>
 constexpr int kStageBytes = 64 * D * 2 * 2;   // keys, then values
 constexpr int kAhead = 2;
 
-template <int D, int GP, int R, int WAVES>
+template <int D, int GP, int R>
 __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int nchunk, int j,
                                                  int row_base, const Partials& part, float scale_log2e, char* lds) {
   constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32, CPL = D / 4, PPT = 32 / GP, TPR = 64 / PPT;
@@ -405,12 +474,10 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     return GP == 16 ? __builtin_amdgcn_readlane(pg_valid, (at + s % 2) & 63) : __builtin_amdgcn_readlane(pg_valid, at & 63) - 16 * (s % 2);
   };
 
-  constexpr bool kBoth = WAVES == 4;
   struct Raw {
-    uint32_t c[kBoth ? 2 * W : W], vs[4], ks;   // codes of keys and values, or of those that this wavefront brings
+    uint32_t c[W], vs[4], ks;   // codes of keys or of values
   };
-  constexpr int kV = kBoth ? W : 0;
-  const bool has_keys = kBoth || wave < 4;
+  const bool has_keys = wave < 4;
   const int mysub = wave & 3;
   auto load_stage = [&](Raw& x, int i) {   // (past the end: the pool's first page, as nothing depends on it)
     const int at = ((2 * i + mysub / 2) * PPT + (GP == 16 ? mysub % 2 : 0)) & 63;
@@ -419,16 +486,8 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     const uint8_t* sc = pk.scales + tile * (2 * GP * J);
     const uint8_t* keys = pk.k + tile * kTileBytes + (row + l16) * (D / 2) + qd * (CPL / 2);
     const uint8_t* values = pk.v + tile * kTileBytes + ((row / 4 + qd) * 16 + l16) * (J * 4);
-    uint32_t w[W];
-    load_dwords<W>(has_keys ? keys : values, w);
-#pragma unroll
-    for (int k = 0; k < W; ++k) x.c[k] = w[k];
-    if constexpr (kBoth) {
-      load_dwords<W>(values, w);
-#pragma unroll
-      for (int k = 0; k < W; ++k) x.c[W + k] = w[k];
-    }
-    x.ks = sc[(row + l16) * J + qd * CPL / 32];   // (with eight wavefronts each has one of the two in vain: no branch around a load)
+    load_dwords<W>(has_keys ? keys : values, x.c);
+    x.ks = sc[(row + l16) * J + qd * CPL / 32];   // (one of the two in vain: no branch around a load)
     load_scales<J>(sc + GP * J + (row + qd * 4) * J, x.vs);
   };
   auto convert_stage = [&](Raw& x, int i, char* buf) {
@@ -439,7 +498,7 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
         *reinterpret_cast<uint4*>(buf + ((mysub * KS + ks) * 64 + lane) * 16) =
             make_uint4(codes_to_bf16<0>(x.c[ks], scale), codes_to_bf16<1>(x.c[ks], scale), codes_to_bf16<2>(x.c[ks], scale), codes_to_bf16<3>(x.c[ks], scale));
     }
-    if (kBoth || !has_keys) {
+    if (!has_keys) {
       const int valid = valid_of(i, mysub);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.vs[e] = qd * 4 + e < valid ? x.vs[e] : 0u;   // (see the other form)
@@ -447,7 +506,7 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
 #pragma unroll
       for (int g = 0; g < J; ++g) {
         uint2 lo, hi;
-        value_operands(x.c[kV + g], x.vs, g, lo, hi);
+        value_operands(x.c[g], x.vs, g, lo, hi);
         *reinterpret_cast<uint2*>(v + (2 * g) * 1024) = lo;
         *reinterpret_cast<uint2*>(v + (2 * g + 1) * 1024) = hi;
       }
@@ -547,80 +606,76 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     for (int i = 0; i < ne; i += 2) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        if (i + k >= ne) break;
-        // stage i + k is in buffer k, the next one goes to the other
-        if (i + k + 1 < ne) convert_stage(raw[(k + 1) % kAhead], i + k + 1, lds + (1 - k) * kStageBytes<D>);
+        // Stage i + k is in buffer k, the next one goes to the other.  (Whether there is one or not: loads behind a branch, or a use of theirs,
+        // would be waited for where the branches join.)
+        convert_stage(raw[(k + 1) % kAhead], i + k + 1, lds + (1 - k) * kStageBytes<D>);
         load_stage(raw[(k + 1) % kAhead], i + k + 1 + kAhead);
-        if (has_rows) compute_stage(i + k, lds + k * kStageBytes<D>, n0 + i + k == 0);
+        if (has_rows && i + k < ne) compute_stage(i + k, lds + k * kStageBytes<D>, n0 + i + k == 0);
         __syncthreads();
       }
     }
   }
 
+  float l_row[R];
+#pragma unroll
+  for (int mt = 0; mt < R; ++mt) l_row[mt] = over_lane_groups_sum(l_run[mt]);
   const uint32_t item = (uint32_t)head * nchunk + chunk;
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) {
-    const float l = over_lane_groups_sum(l_run[mt]);
     const int r = row0 + mt * 16 + l16;
     if (r >= M) continue;
     const uint32_t prow = item * part.rows + r;
     if (qd == 0) {
       part.m[prow] = m_run[mt];
-      part.l[prow] = l;
+      part.l[prow] = l_row[mt];
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + nt * 16 + qd * 4) = o[mt][nt];
   }
 }
 
-// Up to 32 rows: the form whose wavefronts deal the tiles out.
-constexpr int kDealtRows = 32;
-template <int R, int D>
-constexpr int packed_lds_bytes() { return 4 * (R * (D / 16) * 256 + 2 * R * 16) * (int)sizeof(float); }
-
-// Rows that the host knows: blocks of R row tiles.
-template <int D, int GP, int R, int NQ>
-__global__ __launch_bounds__(256) void packed_attn_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
+// Rows that the host knows: blocks of SETS * R row tiles.
+template <int D, int GP, int R, int NQ, int SETS = 1>
+__global__ __launch_bounds__(128 * kSlots) void packed_attn_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
+                                                                   float scale_log2e) {
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  packed_attn_body<D, GP, R, NQ, SETS>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (SETS * R * 16), part, scale_log2e, lds);
+}
+// ... blocks of 8 * R row tiles.
+template <int D, int GP, int R>
+__global__ __launch_bounds__(512) void packed_rows_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
                                                           float scale_log2e) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  packed_attn_body<D, GP, R, NQ, 3>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (R * 16), part, scale_log2e, lds);
-}
-// ... blocks of WAVES * R row tiles.
-template <int D, int GP, int R, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void packed_rows_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
-                                                                 float scale_log2e) {
-  extern __shared__ __attribute__((aligned(16))) float lds[];
-  packed_rows_body<D, GP, R, WAVES>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (WAVES * R * 16), part, scale_log2e,
-                                    reinterpret_cast<char*>(lds));
+  packed_rows_body<D, GP, R>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (128 * R), part, scale_log2e, reinterpret_cast<char*>(lds));
 }
 // Rows counted on the device: the form made for the rows a head has, block after block.  (Workgroups of their own for blocks that most
 // heads do not have would take turns with the others in the launch order, which leaves whole dies with nothing else.)
 template <int D, int GP, int NQ>
-__global__ __launch_bounds__(256) void packed_attn_counted_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
-                                                                  float scale_log2e) {
+__global__ __launch_bounds__(128 * kSlots) void packed_attn_counted_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
+                                                                           float scale_log2e) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
+  constexpr int MOST = NQ == 1 ? 4 : 2;
   const int M = min(active_rows(in, kv, sh, blockIdx.z), min(sh.rows_max, part.rows)), j = blockIdx.y;
-  if (M <= 16) {
-    packed_attn_body<D, GP, 1, NQ, 3>(kv, sh, in, pk, nchunk, j, 0, part, scale_log2e, lds);
-  } else if (M <= kDealtRows) {
-    packed_attn_body<D, GP, 2, NQ, 3>(kv, sh, in, pk, nchunk, j, 0, part, scale_log2e, lds);
-  } else {
-    constexpr int kRows = NQ == 1 ? 64 : 32;
-    for (int row0 = 0; row0 < M; row0 += kRows) {
-      if constexpr (NQ == 1)
-        packed_rows_body<D, GP, 1, 4>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, reinterpret_cast<char*>(lds));
+  for (int row0 = 0; row0 < M; row0 += MOST * 16) {
+    const int left = M - row0;
+    if (left <= 16)
+      packed_attn_body<D, GP, 1, NQ>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
+    else if (left <= 32 || MOST == 2)
+      packed_attn_body<D, GP, 2, NQ>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
+    else if constexpr (MOST > 2) {
+      if (left <= 48)
+        packed_attn_body<D, GP, 3, NQ>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
       else
-        packed_attn_body<D, GP, 2, NQ, 3>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
-      __syncthreads();   // the LDS is the next block's
+        packed_attn_body<D, GP, 2, NQ, 2>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
     }
+    __syncthreads();   // the LDS is the next block's
   }
 }
 
 typedef void (*PackedKernel)(KvView, Shape, AttnInputs, PackedView, int, int, Partials, float);
 
 // block_rows: query rows of a workgroup; 0: all of them, counted on the device
-template <int D, int GP>
-static hipError_t launch_one(PackedKernel kern, bool& attr_set, int waves, int lds_bytes, int block_rows, hipStream_t st, const KvView& kv, const Shape& sh,
+static hipError_t launch_one(PackedKernel kern, bool& attr_set, int lds_bytes, int block_rows, hipStream_t st, const KvView& kv, const Shape& sh,
                              int batch, const AttnInputs& in, const PackedView& pk, int nchunk, int rows, const Partials& part) {
   if (lds_bytes > 48 * 1024 && !attr_set) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
@@ -628,27 +683,28 @@ static hipError_t launch_one(PackedKernel kern, bool& attr_set, int waves, int l
     attr_set = true;
   }
   const int nrb = block_rows ? (rows + block_rows - 1) / block_rows : 1;
-  kern<<<dim3(nchunk, sh.Hkv * nrb, batch), 64 * waves, lds_bytes, st>>>(kv, sh, in, pk, nchunk, nrb, part, sh.sm_scale * 1.4426950408889634f);
+  kern<<<dim3(nchunk, sh.Hkv * nrb, batch), 512, lds_bytes, st>>>(kv, sh, in, pk, nchunk, nrb, part, sh.sm_scale * 1.4426950408889634f);
   return hipGetLastError();
 }
 
 template <int D, int GP>
 static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
                             int nchunk, int rows, bool known, const Partials& part) {
-  static bool attr_set[9];   // per kernel
-  auto go = [&](int which, PackedKernel kern, int waves, int lds_bytes, int block_rows) {
-    return launch_one<D, GP>(kern, attr_set[which], waves, lds_bytes, block_rows, st, kv, sh, batch, in, pk, nchunk, rows, part);
+  static bool attr_set[10];   // per kernel
+  auto go = [&](int which, PackedKernel kern, int lds_bytes, int block_rows) {
+    return launch_one(kern, attr_set[which], lds_bytes, block_rows, st, kv, sh, batch, in, pk, nchunk, rows, part);
   };
-  constexpr int kDealt1 = packed_lds_bytes<1, D>(), kDealt2 = packed_lds_bytes<2, D>(), kStaged = 2 * kStageBytes<D>;
   if (dtype != LOSA_BF16) {
-    if (rows <= 16) return go(0, packed_attn_kernel<D, GP, 1, 3>, 4, kDealt1, 16);
-    return known ? go(1, packed_attn_kernel<D, GP, 2, 3>, 4, kDealt2, 32) : go(2, packed_attn_counted_kernel<D, GP, 3>, 4, kDealt2, 0);
+    if (rows <= 16) return go(0, packed_attn_kernel<D, GP, 1, 3>, DealtLds<1, D, 3>::kBytes, 16);
+    return known ? go(1, packed_attn_kernel<D, GP, 2, 3>, DealtLds<2, D, 3>::kBytes, 32)
+                 : go(2, packed_attn_counted_kernel<D, GP, 3>, DealtLds<2, D, 3>::kBytes, 0);
   }
-  if (rows <= 16) return go(3, packed_attn_kernel<D, GP, 1, 1>, 4, kDealt1, 16);
-  if (!known) return go(4, packed_attn_counted_kernel<D, GP, 1>, 4, kStaged > kDealt2 ? kStaged : kDealt2, 0);
-  if (rows <= kDealtRows) return go(5, packed_attn_kernel<D, GP, 2, 1>, 4, kDealt2, 32);
-  if (rows <= 64) return go(6, packed_rows_kernel<D, GP, 1, 4>, 4, kStaged, 64);
-  return rows <= 128 ? go(7, packed_rows_kernel<D, GP, 1, 8>, 8, kStaged, 128) : go(8, packed_rows_kernel<D, GP, 2, 8>, 8, kStaged, 256);
+  if (rows <= 16) return go(3, packed_attn_kernel<D, GP, 1, 1>, DealtLds<1, D, 1>::kBytes, 16);
+  if (!known) return go(4, packed_attn_counted_kernel<D, GP, 1>, std::max(DealtLds<3, D, 1>::kBytes, DealtLds<2, D, 1, 2>::kBytes), 0);
+  if (rows <= 32) return go(5, packed_attn_kernel<D, GP, 2, 1>, DealtLds<2, D, 1>::kBytes, 32);
+  if (rows <= 48) return go(6, packed_attn_kernel<D, GP, 3, 1>, DealtLds<3, D, 1>::kBytes, 48);
+  if (rows <= 64) return go(7, packed_attn_kernel<D, GP, 2, 1, 2>, DealtLds<2, D, 1, 2>::kBytes, 64);
+  return rows <= 128 ? go(8, packed_rows_kernel<D, GP, 1>, 2 * kStageBytes<D>, 128) : go(9, packed_rows_kernel<D, GP, 2>, 2 * kStageBytes<D>, 256);
 }
 
 hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
