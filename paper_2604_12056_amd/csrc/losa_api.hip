@@ -107,6 +107,7 @@ constexpr long kMergedShares = 64;        // shares of a row that the merge kern
 constexpr long kFewPartials = 4096;       // rows of partials in all that a launch may have for a share per two tiles
 constexpr long kFloatGroups = 2;          // float-mode workgroups per bfloat16 attention workgroup aimed at: two fit a CU
 constexpr long kScoreRound = 5L * 256;    // scoring workgroups counted as one round: four per CU are resident, a quarter more start as those end
+constexpr int kLeastTiles = 8;            // tiles of a share of the attention over a 4-bit cache: one for each wavefront
 constexpr int kSparseRows = 64;           // query rows per KV head up to which the split-pages work shape is used
 
 thread_local char g_create_err[256] = "";
@@ -512,31 +513,30 @@ losa_status sparse_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, in
 }
 
 // The same over a 4-bit cache.
-losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, const PackedView& pk, int batch, int max_seq_pages, const void* q,
+losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, const PackedView& pk, int batch, const void* q,
                              const int32_t* active_idx, const int32_t* active_count, const int32_t* sel_pages, const int32_t* sel_count,
                              int cap, int rows_upper, float* o_p, float* lse_p) {
-  const int upper = sel_pages ? (cap < max_seq_pages ? cap : max_seq_pages) : max_seq_pages;
   if (!active_idx) rows_upper = ctx->sh.rows_max;
   const bool known = rows_upper >= 1 && rows_upper <= ctx->sh.rows_max;
   if (!known) rows_upper = ctx->sh.rows_max;
   Partials part = ctx->part;
   part.rows = known ? std::min((rows_upper + 15) / 16 * 16, ctx->sh.rows_max) : ctx->sh.rows_max;
-  // (a count that only the device knows is mostly that of a few active tokens: shares as for one block of rows)
-  const int block = packed_block_rows(ctx->cfg.dtype), row_blocks = known ? (rows_upper + block - 1) / block : 1;
-  const long heads = (long)batch * ctx->sh.Hkv, tiles = ((long)upper * ctx->sh.g + kPackedTile - 1) / kPackedTile;
-  long want = std::min(ctx->target_workgroups / (heads * row_blocks), ctx->part_rows / (heads * part.rows));
-  want = std::min(want, ctx->shares_set ? tiles : (tiles + 7) / 8);   // (a tile for each wavefront)
-  const int nchunk = (int)std::max(want, 1L);
+  // Shares of all lists, while there are partials for them; the union bitmaps, which nothing reads after the scoring, hold the table that says
+  // which partials a list has.
+  const long heads = (long)batch * ctx->sh.Hkv, room = ctx->part_rows / part.rows - heads;
+  const long workgroups = heads <= kPlannedHeads && room >= kTargetWorkgroups / 2 ? std::min(ctx->target_workgroups, room) : 0;
   const AttnInputs in{q, active_idx, active_count, sel_pages, sel_count, cap};
+  const PackedOut out{o_p, lse_p, (int2*)ctx->union_bits};
   hipError_t e;
   {
     StageTimer timer(ctx, st, LOSA_STAGE_ATTN);
-    e = launch_packed_attn(st, ctx->cfg.dtype, kv, ctx->sh, batch, in, pk, nchunk, rows_upper, known, part);
+    e = launch_packed_attn(st, ctx->cfg.dtype, kv, ctx->sh, batch, in, pk, (int)workgroups, ctx->shares_set ? 1 : kLeastTiles, rows_upper, known, part, out);
   }
   if (e != hipSuccess) return hip_fail(ctx, "packed attention launch", e);
+  if (workgroups == 0) return LOSA_OK;
   StageTimer timer(ctx, st, LOSA_STAGE_MERGE);
-  e = launch_attn_merge(st, kv, ctx->sh, batch, in, true, nchunk, part, o_p, lse_p, known ? rows_upper : 0, kPackedTile, kPackedTile);
-  if (e != hipSuccess) return hip_fail(ctx, "attn_merge launch", e);
+  e = launch_packed_join(st, kv, ctx->sh, batch, in, rows_upper, known, part, out);
+  if (e != hipSuccess) return hip_fail(ctx, "packed join launch", e);
   return LOSA_OK;
 }
 
@@ -558,7 +558,7 @@ losa_status step_impl(losa_ctx* ctx, hipStream_t st, const KvView& view, const P
   if (step_index < 0) return fail(ctx, LOSA_ERR_INVALID_ARG, "step_index is negative");
   if (!q || !o_p || !lse_p) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_step: NULL pointer");
   if (step_index == 0)
-    return pk ? packed_attn_impl(ctx, st, view, *pk, batch, msp, q, nullptr, nullptr, nullptr, nullptr, 0, 0, (float*)o_p, lse_p)
+    return pk ? packed_attn_impl(ctx, st, view, *pk, batch, q, nullptr, nullptr, nullptr, nullptr, 0, 0, (float*)o_p, lse_p)
               : sparse_attn_impl(ctx, st, view, batch, msp, q, nullptr, nullptr, nullptr, nullptr, 0, 0, (float*)o_p, lse_p);
   if (!h_cur || !h_prev) return fail(ctx, LOSA_ERR_INVALID_ARG, "losa_step: h_cur / h_prev are NULL");
   if (topk_pages < 1 || topk_pages > ctx->cfg.max_topk_pages)
@@ -613,7 +613,7 @@ losa_status step_impl(losa_ctx* ctx, hipStream_t st, const KvView& view, const P
                          union_in_attn ? ctx->union_bits : nullptr);
   if (s != LOSA_OK) return s;
   if (pk)
-    return packed_attn_impl(ctx, st, view, *pk, batch, msp, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc, cap, rows_upper,
+    return packed_attn_impl(ctx, st, view, *pk, batch, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc, cap, rows_upper,
                             (float*)o_p, lse_p);
   return sparse_attn_impl(ctx, st, view, batch, msp, q, ctx->active_idx, ctx->active_count, ctx->sel_pages, sc,
                           cap, rows_upper, (float*)o_p, lse_p, union_in_attn ? &uni : nullptr, topk_pages);
@@ -917,7 +917,7 @@ losa_status losa_sparse_attn_packed(losa_ctx* ctx, void* stream, const losa_pack
   losa_status s = check_packed(ctx, kv, false, &msp, &view, &pk);
   if (s == LOSA_OK) s = check_attn_lists(ctx, "losa_sparse_attn_packed", q, active_idx, active_count, sel_pages, sel_count, cap, o_p, lse_p);
   if (s != LOSA_OK) return s;
-  return packed_attn_impl(ctx, as_stream(stream), view, pk, kv->batch, msp, q, active_idx, active_count, sel_pages, sel_count, cap,
+  return packed_attn_impl(ctx, as_stream(stream), view, pk, kv->batch, q, active_idx, active_count, sel_pages, sel_count, cap,
                           /*rows_upper=*/0, (float*)o_p, lse_p);
 }
 

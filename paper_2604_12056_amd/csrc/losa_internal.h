@@ -73,6 +73,12 @@ __device__ __forceinline__ Sequence sequence(const KvView& kv, const Shape& sh, 
   return {base, tokens, max(0, min(min(end - base, filled), min(sh.max_pages, kv.seq_page_limit)))};
 }
 
+// The same for a lane's own b: no scalar loads.
+__device__ __forceinline__ Sequence sequence_of(const KvView& kv, const Shape& sh, int b) {
+  const int base = kv.page_indptr[b], tokens = kv.seq_lens[b], filled = (tokens + sh.g - 1) >> (sh.g == 16 ? 4 : 5);
+  return {base, tokens, max(0, min(min(kv.page_indptr[b + 1] - base, filled), min(sh.max_pages, kv.seq_page_limit)))};
+}
+
 // Split-K partials of the attention: item = ((b*Hkv + j)*nchunk + c), row r < rows.
 struct Partials {
   float* o;   // [items, rows, d]   un-normalised sum_t exp(s_t - m) v_t
@@ -249,12 +255,19 @@ hipError_t launch_append_packed(hipStream_t st, int dtype, const KvView& kv, con
                                 const Rotation& rot, const PackedView& out);
 hipError_t launch_read_packed(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_tokens, const int32_t* indptr,
                               int num_tokens, const PackedView& in, void* k_out, void* v_out);
-// Tiles of 32 tokens are dealt round-robin to `nchunk` work items; partials in rows, references in log2 units.
+// Every workgroup has an equal share of all lists' tiles of 32 tokens (packed_attn.hip), at least least_tiles of them; workgroups == 0: a list each, which
+// leaves nothing to join.  Partials: item workgroup + head, in rows, references in log2 units.
 // rows: an upper bound on the query rows of a KV head; rows_known: the number itself.
-constexpr int kPackedTile = 32;
-inline int packed_block_rows(int dtype) { return dtype == LOSA_BF16 ? 256 : 32; }   // query rows of a workgroup, at most
-hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
-                              int nchunk, int rows, bool rows_known, const Partials& part);
+constexpr int kPlannedHeads = 256;
+struct PackedOut {
+  float* o_p;
+  float* lse_p;
+  int2* table;   // [heads]: a list's first item and their number (1: finished in the attention kernel, 0: it has no page)
+};
+hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk, int workgroups,
+                              int least_tiles, int rows, bool rows_known, const Partials& part, const PackedOut& out);
+hipError_t launch_packed_join(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, int rows, bool rows_known, const Partials& part,
+                              const PackedOut& out);
 
 // ---- block_merge.hip
 hipError_t launch_block_merge(hipStream_t st, int dtype, const Shape& sh, int batch, const void* q, const void* k_b,

@@ -114,6 +114,117 @@ __device__ __forceinline__ float numerators(const f32x4_t& a, const f32x4_t& b, 
   return sum;
 }
 
+// ---- who does what.  The tiles of all (sequence, KV head) lists, one list behind the other and weighted with what a tile of so many query rows costs, are
+// cut into equal shares, one per workgroup: lists of any lengths keep every compute unit busy to the end.  A share that ends inside a list leaves a
+// partial, and the merge kernel joins a list's partials; a list that lies in one share is finished by its workgroup.
+// Every workgroup works the cut out for itself from the counts (one memory round trip and a prefix sum): lists in the order of their
+// heads, list h at [start, start + tiles * unit).  Tile t is workgroup (start + t * unit) / share's.  The partial of workgroup w for list h is item w + h.
+// Beyond kPlannedHeads lists every one has a workgroup of its own.
+struct Segment {
+  int b, j, head, M;       // M: query rows
+  int pages, t0, t1;       // listed pages, and the tiles [t0, t1) of them that are this workgroup's
+  int item;                // partial; negative: the list is finished here
+};
+__device__ __forceinline__ int row_blocks(int M, int most) { return (M + most - 1) / most; }
+// What a tile costs: converting it once per block of rows, and every 16 rows about as much as half of that.
+__device__ __forceinline__ int unit_cost(int M, int block) { return M <= 0 ? 0 : 2 * row_blocks(M, block) + row_blocks(M, 16); }
+
+// BLOCK: query rows that convert a tile once.  f(segment) for every list of this workgroup, in order.
+template <int GP, int BLOCK, typename F>
+__device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& sh, const AttnInputs& in, const Partials& part, const PackedOut& out, int heads,
+                                                 int workgroups, int least_tiles, int* plan, F f) {
+  constexpr int PPT = 32 / GP;
+  const int lane = threadIdx.x & 63;
+  auto list_of = [&](int h, int& M, int& pages) {
+    const int b = h / sh.Hkv;
+    M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
+    const Sequence seq = sequence_of(kv, sh, b);
+    pages = in.list ? max(0, min(min(in.sel_count[h], in.cap), sh.max_pages)) : seq.pages;
+  };
+  if (workgroups == 0) {   // a list each
+    Segment s;
+    s.head = blockIdx.x;
+    s.b = s.head / sh.Hkv;
+    s.j = s.head % sh.Hkv;
+    list_of(s.head, s.M, s.pages);
+    s.t0 = 0;
+    s.t1 = (s.pages + PPT - 1) / PPT;
+    s.item = -1;
+    if (s.M > 0) f(s);
+    return;
+  }
+  // the plan, [start | tiles | unit | pages] per head in LDS: every wavefront makes it, all of them the same
+  int total = 0, most_unit = 1;
+  for (int h0 = 0; h0 < heads; h0 += 64) {
+    const int h = h0 + lane;
+    int M = 0, pages = 0;
+    if (h < heads) list_of(h, M, pages);
+    const int unit = unit_cost(M, BLOCK), tiles = M > 0 ? (pages + PPT - 1) / PPT : 0, cost = tiles * unit;
+    const int incl = wave_inclusive_scan(cost);
+    if (h < heads) reinterpret_cast<int4*>(plan)[h] = make_int4(total + incl - cost, tiles, unit, pages);
+    total += __builtin_amdgcn_readlane(incl, 63);
+    most_unit = max(most_unit, (int)wave_max_u32((uint32_t)unit));
+  }
+  wave_lds_fence();
+  const int w = blockIdx.x, share = max((total + workgroups - 1) / workgroups, least_tiles * most_unit);
+  if (w == 0) {
+    for (int h = threadIdx.x; h < heads; h += blockDim.x) {
+      const int4 p = reinterpret_cast<const int4*>(plan)[h];
+      const int first = p.x / share, last = (p.x + (p.y - 1) * p.z) / share;
+      out.table[h] = make_int2(first + h, p.y > 0 ? last - first + 1 : 0);
+    }
+  }
+  const int begin = w * share, end = begin + share;
+  int first = heads;
+  for (int h0 = 0; h0 < heads; h0 += 64) {   // the first list that reaches into the share
+    const int h = h0 + lane;
+    const int4 p = reinterpret_cast<const int4*>(plan)[min(h, heads - 1)];
+    const unsigned long long in_it = __ballot(h < heads && p.y > 0 && p.x + p.y * p.z > begin);
+    if (in_it) {
+      first = h0 + __builtin_ctzll(in_it);
+      break;
+    }
+  }
+  for (int h = first; h < heads; ++h) {
+    const int4 p = reinterpret_cast<const int4*>(plan)[h];
+    const int start = __builtin_amdgcn_readfirstlane(p.x), tiles = __builtin_amdgcn_readfirstlane(p.y), unit = __builtin_amdgcn_readfirstlane(p.z);
+    if (start >= end) break;
+    if (tiles == 0) continue;
+    Segment s;
+    s.t0 = begin <= start ? 0 : (begin - start + unit - 1) / unit;
+    s.t1 = min(tiles, (end - start + unit - 1) / unit);
+    if (s.t0 >= s.t1) continue;
+    s.head = h;
+    s.b = h / sh.Hkv;
+    s.j = h - s.b * sh.Hkv;
+    s.M = min(active_rows(in, kv, sh, s.b), min(sh.rows_max, part.rows));
+    s.pages = __builtin_amdgcn_readfirstlane(p.w);
+    s.item = s.t0 == 0 && s.t1 == tiles ? -1 : w + h;
+    f(s);
+  }
+}
+
+// A vector of four channels of row r of a segment, numerators against `m` with sum `l`: a partial's, or the finished output.
+template <int D>
+__device__ __forceinline__ void store_state(const Shape& sh, const AttnInputs& in, const Partials& part, const PackedOut& out, const Segment& s, int r, int channel,
+                                            f32x4_t acc, float m, float l) {
+  if (s.item >= 0) {
+    const uint32_t prow = (uint32_t)s.item * part.rows + r;
+    if (channel == 0) {
+      part.m[prow] = m;
+      part.l[prow] = l;
+    }
+    *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + channel) = acc;
+    return;
+  }
+  const int a = row_token(sh, r), tok = in.active_idx ? in.active_idx[(size_t)s.b * sh.B + a] : a;
+  if ((unsigned)tok >= (unsigned)sh.B) return;
+  const size_t orow = ((size_t)s.b * sh.B + tok) * sh.Hq + s.j * sh.G + (r - a * sh.G);
+  const bool any = m > -1.0e29f || l != l;   // no valid token at all: the neutral element of a merge.  (Scores that are all NaN move no reference)
+  *reinterpret_cast<f32x4_t*>(out.o_p + orow * D + channel) = any ? acc / l : (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  if (channel == 0) out.lse_p[orow] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
 // Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup of up to 64 rows does.  Its WAVES wavefronts deal the share's tiles out, two
 // wavefronts to a SIMD, so that one's matrix products run beside the other's vector work.  That takes 256 registers a lane at most:
 //   a tile's codes have no second buffer: the next tile's keys are requested when this one's have been converted, its values after
@@ -130,8 +241,8 @@ struct DealtLds {
   static constexpr int kBytes = (kQueryFloats + SETS * kSlots * kState) * (int)sizeof(float);
 };
 template <int D, int GP, int R, int NQ, int SETS = 1>
-__device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int nchunk, int j,
-                                                 int row_base, const Partials& part, float scale_log2e, float* lds) {
+__device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, const Segment& seg, int row_base,
+                                                 const Partials& part, const PackedOut& out, float scale_log2e, float* lds) {
   constexpr int WAVES = 2 * kSlots / SETS;   // of a set
   constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32;   // products per score, channel tiles, groups, dwords a lane reads of a subtile
   constexpr int CPL = D / 4;                                        // channels of a token that a lane has
@@ -140,25 +251,21 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
   typedef DealtLds<R, D, NQ, SETS> Lds;
   static_assert(SETS == 1 || !Lds::kQueries, "the sets' queries are not the same");
   constexpr bool kTight = D == 128 && Lds::kQueries;   // registers are short
-  const int lane = threadIdx.x & 63, in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_group % WAVES, set = in_group / WAVES;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));   // (what derives from it is worked out per segment, not kept in registers over all of them)
+  const int in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_group % WAVES, set = in_group / WAVES;
   const int l16 = lane & 15, qd = lane >> 4;
-  const int chunk = blockIdx.x, b = blockIdx.z, head = b * sh.Hkv + j, row0 = row_base + set * (R * 16);
-
+  const int b = seg.b, j = seg.j, M = seg.M, row0 = row_base + set * (R * 16);
   const Sequence seq = sequence(kv, sh, b);
-  const int M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
-  const int U = min(in.list ? min(in.sel_count[head], in.cap) : seq.pages, sh.max_pages);
-  const int ntiles = (U + PPT - 1) / PPT;
-  if (row_base >= M || chunk >= ntiles) return;
-  // tiles are dealt round-robin to the workgroups, and a workgroup's to its wavefronts
-  const int tfirst = chunk + nchunk * wave, tstep = nchunk * WAVES;
-  const int ntw = tfirst < ntiles ? (ntiles - 1 - tfirst) / tstep + 1 : 0;
+  // tiles are dealt round-robin to the wavefronts
+  const int tfirst = seg.t0 + wave, ntw = tfirst < seg.t1 ? (seg.t1 - 1 - tfirst) / WAVES + 1 : 0;
 
   // ---- pages of this wavefront's next TPR tiles, one per lane
   int pg_phys = 0, pg_valid = 0;
   auto fetch_pages = [&](int n0) {
-    const int at = (tfirst + (n0 + lane / PPT) * tstep) * PPT + lane % PPT;
+    const int at = (tfirst + (n0 + lane / PPT) * WAVES) * PPT + lane % PPT;
     int logical = -1, phys = -1;
-    if (at < U) logical = in.list ? in.list[(size_t)head * in.cap + at] : at;
+    if (at < seg.pages) logical = in.list ? in.list[(size_t)seg.head * in.cap + at] : at;
     if ((unsigned)logical < (unsigned)seq.pages) phys = kv.page_indices[seq.base + logical];
     const bool ok = (unsigned)phys < (unsigned)kv.num_pages;
     pg_phys = ok ? phys : 0;
@@ -385,7 +492,6 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
     publish();
   }
   __syncthreads();
-  const uint32_t item = (uint32_t)head * nchunk + chunk;
   for (int piece = in_group; piece < SETS * R * NT; piece += SETS * WAVES) {
     const int of = piece / (R * NT), vec = piece % (R * NT), mt = vec / NT, nt = vec % NT, r = row_base + of * (R * 16) + mt * 16 + l16;
     if (r >= M) continue;
@@ -407,13 +513,9 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
       l_all = fmaf(l[w], wgt, l_all);
       acc += x[w] * wgt;
     }
-    const uint32_t prow = item * part.rows + r;
-    if (nt == 0 && qd == 0) {
-      part.m[prow] = m_all;
-      part.l[prow] = l_all;
-    }
-    *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + nt * 16 + qd * 4) = acc;
+    store_state<D>(sh, in, part, out, seg, r, nt * 16 + qd * 4, acc, m_all, l_all);
   }
+  __syncthreads();   // the LDS is the next segment's
 }
 
 // ---- more than 64 query rows: the eight wavefronts of a workgroup have R*16 rows each and share the tiles.
@@ -426,21 +528,17 @@ constexpr int kStageBytes = 64 * D * 2 * 2;   // keys, then values
 constexpr int kAhead = 2;
 
 template <int D, int GP, int R>
-__device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int nchunk, int j,
-                                                 int row_base, const Partials& part, float scale_log2e, char* lds) {
+__device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, const Segment& seg, int row_base,
+                                                 const Partials& part, const PackedOut& out, float scale_log2e, char* lds) {
   constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32, CPL = D / 4, PPT = 32 / GP, TPR = 64 / PPT;
   constexpr int kTileBytes = GP * D / 2;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));   // (see the other form)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, qd = lane >> 4;
-  const int chunk = blockIdx.x, b = blockIdx.z, head = b * sh.Hkv + j;
-  const int row0 = row_base + wave * (R * 16);
-
+  const int b = seg.b, j = seg.j, M = seg.M, row0 = row_base + wave * (R * 16);
   const Sequence seq = sequence(kv, sh, b);
-  const int M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
-  const int U = min(in.list ? min(in.sel_count[head], in.cap) : seq.pages, sh.max_pages);
-  const int ntiles = (U + PPT - 1) / PPT;
-  if (row_base >= M || chunk >= ntiles) return;
-  const int mytiles = (ntiles - 1 - chunk) / nchunk + 1, stages = (mytiles + 1) / 2;
+  const int stages = (seg.t1 - seg.t0 + 1) / 2;
 
   bf16x8_t qf[R][KS];
 #pragma unroll
@@ -460,9 +558,9 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
   // pages of the share's next TPR tiles, one per lane
   int pg_phys = 0, pg_valid = 0;
   auto fetch_pages = [&](int n0) {
-    const int at = (chunk + (n0 + lane / PPT) * nchunk) * PPT + lane % PPT;
+    const int tile = seg.t0 + n0 + lane / PPT, at = tile * PPT + lane % PPT;
     int logical = -1, phys = -1;
-    if (at < U) logical = in.list ? in.list[(size_t)head * in.cap + at] : at;
+    if (tile < seg.t1 && at < seg.pages) logical = in.list ? in.list[(size_t)seg.head * in.cap + at] : at;
     if ((unsigned)logical < (unsigned)seq.pages) phys = kv.page_indices[seq.base + logical];
     const bool ok = (unsigned)phys < (unsigned)kv.num_pages;
     pg_phys = ok ? phys : 0;
@@ -619,102 +717,173 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
   float l_row[R];
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) l_row[mt] = over_lane_groups_sum(l_run[mt]);
-  const uint32_t item = (uint32_t)head * nchunk + chunk;
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) {
     const int r = row0 + mt * 16 + l16;
     if (r >= M) continue;
-    const uint32_t prow = item * part.rows + r;
-    if (qd == 0) {
-      part.m[prow] = m_run[mt];
-      part.l[prow] = l_row[mt];
-    }
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + nt * 16 + qd * 4) = o[mt][nt];
+    for (int nt = 0; nt < NT; ++nt) store_state<D>(sh, in, part, out, seg, r, nt * 16 + qd * 4, o[mt][nt], m_run[mt], l_row[mt]);
   }
 }
 
-// Rows that the host knows: blocks of SETS * R row tiles.
+#define LOSA_PACKED_ARGS KvView kv, Shape sh, AttnInputs in, PackedView pk, Partials part, PackedOut out, float scale_log2e, int heads, int workgroups, int least_tiles
+// Rows that the host knows: blocks of SETS * R row tiles, one after the other.
 template <int D, int GP, int R, int NQ, int SETS = 1>
-__global__ __launch_bounds__(128 * kSlots) void packed_attn_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
-                                                                   float scale_log2e) {
+__global__ __launch_bounds__(128 * kSlots) void packed_attn_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  packed_attn_body<D, GP, R, NQ, SETS>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (SETS * R * 16), part, scale_log2e, lds);
+  constexpr int kRows = SETS * R * 16;
+  int* plan = reinterpret_cast<int*>(lds) + DealtLds<R, D, NQ, SETS>::kBytes / 4;
+  for_each_segment<GP, kRows>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
+    for (int row0 = 0; row0 < s.M; row0 += kRows) packed_attn_body<D, GP, R, NQ, SETS>(kv, sh, in, pk, s, row0, part, out, scale_log2e, lds);
+  });
 }
 // ... blocks of 8 * R row tiles.
 template <int D, int GP, int R>
-__global__ __launch_bounds__(512) void packed_rows_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
-                                                          float scale_log2e) {
+__global__ __launch_bounds__(512) void packed_rows_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  packed_rows_body<D, GP, R>(kv, sh, in, pk, nchunk, (int)blockIdx.y / nrb, (int)(blockIdx.y % nrb) * (128 * R), part, scale_log2e, reinterpret_cast<char*>(lds));
+  constexpr int kRows = 128 * R;
+  int* plan = reinterpret_cast<int*>(lds) + 2 * kStageBytes<D> / 4;
+  for_each_segment<GP, kRows>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
+    for (int row0 = 0; row0 < s.M; row0 += kRows) packed_rows_body<D, GP, R>(kv, sh, in, pk, s, row0, part, out, scale_log2e, reinterpret_cast<char*>(lds));
+  });
 }
-// Rows counted on the device: the form made for the rows a head has, block after block.  (Workgroups of their own for blocks that most
-// heads do not have would take turns with the others in the launch order, which leaves whole dies with nothing else.)
+// Rows counted on the device: the form made for the rows a head has, block after block.
+template <int NQ>
+constexpr int kCountedRows = NQ == 1 ? 64 : 32;
+template <int D, int NQ>
+constexpr int kCountedBytes = NQ == 1 ? std::max(DealtLds<3, D, 1>::kBytes, DealtLds<2, D, 1, 2>::kBytes) : DealtLds<2, D, NQ>::kBytes;
 template <int D, int GP, int NQ>
-__global__ __launch_bounds__(128 * kSlots) void packed_attn_counted_kernel(KvView kv, Shape sh, AttnInputs in, PackedView pk, int nchunk, int nrb, Partials part,
-                                                                           float scale_log2e) {
+__global__ __launch_bounds__(128 * kSlots) void packed_attn_counted_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  constexpr int MOST = NQ == 1 ? 4 : 2;
-  const int M = min(active_rows(in, kv, sh, blockIdx.z), min(sh.rows_max, part.rows)), j = blockIdx.y;
-  for (int row0 = 0; row0 < M; row0 += MOST * 16) {
-    const int left = M - row0;
-    if (left <= 16)
-      packed_attn_body<D, GP, 1, NQ>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
-    else if (left <= 32 || MOST == 2)
-      packed_attn_body<D, GP, 2, NQ>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
-    else if constexpr (MOST > 2) {
-      if (left <= 48)
-        packed_attn_body<D, GP, 3, NQ>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
-      else
-        packed_attn_body<D, GP, 2, NQ, 2>(kv, sh, in, pk, nchunk, j, row0, part, scale_log2e, lds);
+  int* plan = reinterpret_cast<int*>(lds) + kCountedBytes<D, NQ> / 4;
+  for_each_segment<GP, kCountedRows<NQ>>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
+    for (int row0 = 0; row0 < s.M; row0 += kCountedRows<NQ>) {
+      const int left = s.M - row0;
+      if (left <= 16)
+        packed_attn_body<D, GP, 1, NQ>(kv, sh, in, pk, s, row0, part, out, scale_log2e, lds);
+      else if (left <= 32 || NQ > 1)
+        packed_attn_body<D, GP, 2, NQ>(kv, sh, in, pk, s, row0, part, out, scale_log2e, lds);
+      else if constexpr (NQ == 1) {
+        if (left <= 48)
+          packed_attn_body<D, GP, 3, NQ>(kv, sh, in, pk, s, row0, part, out, scale_log2e, lds);
+        else
+          packed_attn_body<D, GP, 2, NQ, 2>(kv, sh, in, pk, s, row0, part, out, scale_log2e, lds);
+      }
     }
-    __syncthreads();   // the LDS is the next block's
+  });
+}
+
+// ---- joins a list's partials: a workgroup per row (of a few, in turn), 1024 / D lanes of items times D / 4 channel quads, eight items of a lane at
+// once; sums in a fixed order.
+template <int D>
+__global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, AttnInputs in, Partials part, PackedOut out) {
+  constexpr int C4 = D / 4, CL = 256 / C4, KB = 8;
+  __shared__ __attribute__((aligned(16))) float4 red[CL][C4];
+  __shared__ float2 stats[CL];
+  const int tid = threadIdx.x, cl = tid / C4, c4 = tid % C4, head = blockIdx.y, b = head / sh.Hkv, j = head - b * sh.Hkv;
+  const int2 table = out.table[head];
+  const int M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
+  if (table.y == 1) return;   // finished already
+  for (int r = blockIdx.x; r < M; r += gridDim.x) {
+    const int a = row_token(sh, r), tok = in.active_idx ? in.active_idx[(size_t)b * sh.B + a] : a;
+    float m = kNegBig, l = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = cl; i0 < table.y; i0 += CL * KB) {
+      float mk[KB], lk[KB];
+      f32x4_t x[KB];
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        const uint32_t prow = (uint32_t)(table.x + min(i0 + CL * k, table.y - 1)) * part.rows + r;
+        mk[k] = part.m[prow];
+        lk[k] = part.l[prow];
+        x[k] = reinterpret_cast<const f32x4_t*>(part.o + (size_t)prow * D)[c4];
+      }
+      float m_new = m;
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        if (i0 + CL * k >= table.y) mk[k] = kNegBig, lk[k] = 0.f, x[k] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        m_new = fmaxf(m_new, mk[k]);
+      }
+      const float keep = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= keep;
+      acc *= keep;
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        const float wgt = __builtin_amdgcn_exp2f(mk[k] - m);
+        l = fmaf(lk[k], wgt, l);
+        acc += x[k] * wgt;
+      }
+    }
+    red[cl][c4] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    if (c4 == 0) stats[cl] = make_float2(m, l);
+    __syncthreads();
+    if (tid < C4 && (unsigned)tok < (unsigned)sh.B) {
+      float m_all = kNegBig, l_all = 0.f;
+      f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < CL; ++k) m_all = fmaxf(m_all, stats[k].x);
+#pragma unroll
+      for (int k = 0; k < CL; ++k) {
+        const float wgt = __builtin_amdgcn_exp2f(stats[k].x - m_all);
+        const float4 x = red[k][c4];
+        l_all = fmaf(stats[k].y, wgt, l_all);
+        o += (f32x4_t){x.x, x.y, x.z, x.w} * wgt;
+      }
+      Segment s;
+      s.b = b;
+      s.j = j;
+      s.item = -1;
+      store_state<D>(sh, in, part, out, s, r, c4 * 4, o, m_all, l_all);
+    }
+    __syncthreads();   // the LDS is the next row's
   }
 }
 
-typedef void (*PackedKernel)(KvView, Shape, AttnInputs, PackedView, int, int, Partials, float);
-
-// block_rows: query rows of a workgroup; 0: all of them, counted on the device
-static hipError_t launch_one(PackedKernel kern, bool& attr_set, int lds_bytes, int block_rows, hipStream_t st, const KvView& kv, const Shape& sh,
-                             int batch, const AttnInputs& in, const PackedView& pk, int nchunk, int rows, const Partials& part) {
-  if (lds_bytes > 48 * 1024 && !attr_set) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
-    if (e != hipSuccess) return e;
-    attr_set = true;
-  }
-  const int nrb = block_rows ? (rows + block_rows - 1) / block_rows : 1;
-  kern<<<dim3(nchunk, sh.Hkv * nrb, batch), 512, lds_bytes, st>>>(kv, sh, in, pk, nchunk, nrb, part, sh.sm_scale * 1.4426950408889634f);
-  return hipGetLastError();
-}
+typedef void (*PackedKernel)(LOSA_PACKED_ARGS);
 
 template <int D, int GP>
-static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
-                            int nchunk, int rows, bool known, const Partials& part) {
-  static bool attr_set[10];   // per kernel
-  auto go = [&](int which, PackedKernel kern, int lds_bytes, int block_rows) {
-    return launch_one(kern, attr_set[which], lds_bytes, block_rows, st, kv, sh, batch, in, pk, nchunk, rows, part);
+static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int heads, int workgroups,
+                            int least_tiles, int rows, bool known, const Partials& part, const PackedOut& out) {
+  auto go = [&](PackedKernel kern, int lds_bytes, bool& attr_set) {
+    const int all = lds_bytes + (workgroups ? heads * 16 : 0);   // the plan behind the kernel's own
+    if (!attr_set) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes + kPlannedHeads * 16);
+      if (e != hipSuccess) return e;
+      attr_set = true;
+    }
+    kern<<<workgroups ? workgroups : heads, 512, all, st>>>(kv, sh, in, pk, part, out, sh.sm_scale * 1.4426950408889634f, heads, workgroups, least_tiles);
+    return hipGetLastError();
   };
+  static bool set[10];   // per kernel
   if (dtype != LOSA_BF16) {
-    if (rows <= 16) return go(0, packed_attn_kernel<D, GP, 1, 3>, DealtLds<1, D, 3>::kBytes, 16);
-    return known ? go(1, packed_attn_kernel<D, GP, 2, 3>, DealtLds<2, D, 3>::kBytes, 32)
-                 : go(2, packed_attn_counted_kernel<D, GP, 3>, DealtLds<2, D, 3>::kBytes, 0);
+    if (rows <= 16) return go(packed_attn_kernel<D, GP, 1, 3>, DealtLds<1, D, 3>::kBytes, set[0]);
+    return known ? go(packed_attn_kernel<D, GP, 2, 3>, DealtLds<2, D, 3>::kBytes, set[1]) : go(packed_attn_counted_kernel<D, GP, 3>, kCountedBytes<D, 3>, set[2]);
   }
-  if (rows <= 16) return go(3, packed_attn_kernel<D, GP, 1, 1>, DealtLds<1, D, 1>::kBytes, 16);
-  if (!known) return go(4, packed_attn_counted_kernel<D, GP, 1>, std::max(DealtLds<3, D, 1>::kBytes, DealtLds<2, D, 1, 2>::kBytes), 0);
-  if (rows <= 32) return go(5, packed_attn_kernel<D, GP, 2, 1>, DealtLds<2, D, 1>::kBytes, 32);
-  if (rows <= 48) return go(6, packed_attn_kernel<D, GP, 3, 1>, DealtLds<3, D, 1>::kBytes, 48);
-  if (rows <= 64) return go(7, packed_attn_kernel<D, GP, 2, 1, 2>, DealtLds<2, D, 1, 2>::kBytes, 64);
-  return rows <= 128 ? go(8, packed_rows_kernel<D, GP, 1>, 2 * kStageBytes<D>, 128) : go(9, packed_rows_kernel<D, GP, 2>, 2 * kStageBytes<D>, 256);
+  if (rows <= 16) return go(packed_attn_kernel<D, GP, 1, 1>, DealtLds<1, D, 1>::kBytes, set[3]);
+  if (!known) return go(packed_attn_counted_kernel<D, GP, 1>, kCountedBytes<D, 1>, set[4]);
+  if (rows <= 32) return go(packed_attn_kernel<D, GP, 2, 1>, DealtLds<2, D, 1>::kBytes, set[5]);
+  if (rows <= 48) return go(packed_attn_kernel<D, GP, 3, 1>, DealtLds<3, D, 1>::kBytes, set[6]);
+  if (rows <= 64) return go(packed_attn_kernel<D, GP, 2, 1, 2>, DealtLds<2, D, 1, 2>::kBytes, set[7]);
+  return rows <= 128 ? go(packed_rows_kernel<D, GP, 1>, 2 * kStageBytes<D>, set[8]) : go(packed_rows_kernel<D, GP, 2>, 2 * kStageBytes<D>, set[9]);
 }
 
-hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk,
-                              int nchunk, int rows, bool rows_known, const Partials& part) {
-  if (batch <= 0 || nchunk <= 0 || rows <= 0) return hipSuccess;
+hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk, int workgroups,
+                              int least_tiles, int rows, bool rows_known, const Partials& part, const PackedOut& out) {
+  const int heads = batch * sh.Hkv;
+  if (heads <= 0 || rows <= 0) return hipSuccess;
+  auto launch = sh.d == 128 ? (sh.g == 16 ? launch_dg<128, 16> : launch_dg<128, 32>) : (sh.g == 16 ? launch_dg<64, 16> : launch_dg<64, 32>);
+  return launch(st, dtype, kv, sh, in, pk, heads, workgroups, least_tiles, rows, rows_known, part, out);
+}
+
+hipError_t launch_packed_join(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, int rows, bool rows_known, const Partials& part,
+                              const PackedOut& out) {
+  const dim3 grid(rows_known ? rows : min(rows, 64), batch * sh.Hkv);   // (rows that only the device counts are mostly few)
   if (sh.d == 128)
-    return sh.g == 16 ? launch_dg<128, 16>(st, dtype, kv, sh, batch, in, pk, nchunk, rows, rows_known, part)
-                      : launch_dg<128, 32>(st, dtype, kv, sh, batch, in, pk, nchunk, rows, rows_known, part);
-  return sh.g == 16 ? launch_dg<64, 16>(st, dtype, kv, sh, batch, in, pk, nchunk, rows, rows_known, part)
-                    : launch_dg<64, 32>(st, dtype, kv, sh, batch, in, pk, nchunk, rows, rows_known, part);
+    packed_join_kernel<128><<<grid, 256, 0, st>>>(kv, sh, in, part, out);
+  else
+    packed_join_kernel<64><<<grid, 256, 0, st>>>(kv, sh, in, part, out);
+  return hipGetLastError();
 }
 
 }  // namespace losa

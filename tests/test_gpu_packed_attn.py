@@ -228,6 +228,43 @@ def test_not_a_number_reaches_its_rows_only():
     rig.close()
 
 
+def test_a_query_that_is_not_a_number_spoils_its_own_rows_only():
+    for lens in ((40, 25), (2000, 0, 900)):
+        rig = Rig(14, 6, 2, 64, 16, 3, lens)
+        want, want_l = rig.run()
+        rig.q_s[1, 4, 7] = 0x7FC0
+        o, l = rig.run()
+        assert bool(torch.isnan(o[1, 4]).all()) and bool(torch.isnan(l[1, 4])) and int(torch.isnan(o).sum()) == 64
+        keep = torch.ones_like(l, dtype=torch.bool)
+        keep[1, 4] = False
+        assert torch.equal(o[keep], want[keep]) and torch.equal(l[keep], want_l[keep])
+        rig.close()
+
+
+@pytest.mark.parametrize("heads,batch", [(3, 70), (8, 40), (2, 200)])
+def test_many_heads(heads, batch):
+    """More lists than one wavefront has lanes, than are planned for, and rows that leave no room for partials."""
+    rng = np.random.default_rng(heads)
+    lens = tuple(int(x) for x in rng.integers(0, 90, batch))
+    rig = Rig(heads, heads, heads, 64, 16, 2, lens)
+    rig.check(*rig.run())
+    active = [sorted(rng.permutation(2)[:rng.integers(0, 3)].tolist()) for _ in range(batch)]
+    lists = [[sorted(rng.permutation(p)[:rng.integers(0, p + 1)].tolist()) for _ in range(heads)] for p in rig.pages]
+    rig.check(*rig.run(active, lists), active, lists)
+    rig.close()
+
+
+def test_lists_of_very_different_lengths_and_rows():
+    rig = Rig(15, 14, 2, 128, 16, 12, (6000, 0, 3, 700, 17))
+    rng = rig.rng
+    for trial in range(3):
+        active = [sorted(rng.permutation(12)[:n].tolist()) for n in ((1, 12, 0, 5, 7), (12, 2, 12, 0, 1), (0, 0, 3, 0, 0))[trial]]
+        rig.check(*rig.run(active), active)
+        lists = [[sorted(rng.permutation(p)[:rng.integers(0, p + 1)].tolist()) for _ in range(2)] for p in rig.pages]
+        rig.check(*rig.run(active, lists), active, lists)
+    rig.close()
+
+
 def test_the_same_call_twice_gives_the_same_bits():
     rig = Rig(12, 28, 4, 128, 16, 32, (3000, 1111))
     active = [[1, 4, 5, 9, 20, 31], [0]]
