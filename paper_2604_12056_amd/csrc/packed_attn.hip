@@ -12,8 +12,8 @@
 //                           permutations pair the tokens up.
 //
 // Numbers: keys are exact in bfloat16, values in half precision.  Probabilities enter the second product as a pair of halves, hi rounded to
-// nearest and lo = p - hi rounded again (22 bits: error 2^-23 of p, against 2^-17 of a bfloat16 pair at the same cost); their sum is kept
-// in float from the unrounded p.  Float mode splits a query into three bfloat16 terms, which hold its 24 bits.
+// nearest and lo = p - hi rounded again (22 bits: error 2^-23 of p, against 2^-17 of a bfloat16 pair at the same cost), and so does their sum,
+// in float.  Float mode splits a query into three bfloat16 terms, which hold its 24 bits.
 // p is taken against a reference 2^7 below the row's maximum that may lag it by 2^8 (see kLag), so p < 2^15 is inside a half's
 // range and what lo cannot hold is below 2^-25, 2^-32 of the largest p.
 #include <math.h>
@@ -38,9 +38,6 @@ constexpr float kLag = 8.0f, kHeadroom = 7.0f;
 __device__ __forceinline__ float over_lane_groups_max(float v) {
   return __uint_as_float(across_rows(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
 }
-__device__ __forceinline__ float over_lane_groups_sum(float v) {
-  return __uint_as_float(across_rows(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
-}
 
 // 16 or 8 bytes of codes per lane, as dwords
 template <int N>
@@ -59,9 +56,15 @@ __device__ __forceinline__ void load_dwords(const uint8_t* p, uint32_t (&w)[N]) 
   }
 }
 
-__device__ __forceinline__ void load_floats8(const float* p, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+template <int N>
+__device__ __forceinline__ void lds_dwords(const char* p, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+  } else {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x, w[1] = x.y;
+  }
 }
 
 // Scale bytes of four consecutive tokens' values: a dword per token, a byte per group.
@@ -82,11 +85,26 @@ __device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t (&w)[4]) 
   }
 }
 
+// The power of two that byte g of a dword stands for, in one instruction (left to itself the compiler makes two of the shift and the mask).
+__device__ __forceinline__ float power_of_byte(uint32_t w, int g) {
+  uint32_t r;
+  const uint32_t places = 23;
+  if (g == 0)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(places), "v"(w));
+  else if (g == 1)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(places), "v"(w));
+  else if (g == 2)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(places), "v"(w));
+  else
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(places), "v"(w));
+  return __uint_as_float(r);
+}
+
 // Group g's codes of four tokens under their scales: the halves of channel tiles 2 g (low codes) and 2 g + 1, tokens side by side.
 __device__ __forceinline__ void value_operands(uint32_t codes, const uint32_t (&scales)[4], int g, uint2& lo, uint2& hi) {
   float f[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) f[e] = power_of((scales[e] >> (8 * g)) & 0xFFu);
+  for (int e = 0; e < 4; ++e) f[e] = power_of_byte(scales[e], g);
   const uint32_t n0 = codes_to_f16<0>(codes, f[0]), n1 = codes_to_f16<1>(codes, f[1]);
   const uint32_t n2 = codes_to_f16<2>(codes, f[2]), n3 = codes_to_f16<3>(codes, f[3]);
   lo.x = __builtin_amdgcn_perm(n1, n0, 0x05040100u);
@@ -95,23 +113,44 @@ __device__ __forceinline__ void value_operands(uint32_t codes, const uint32_t (&
   hi.y = __builtin_amdgcn_perm(n3, n2, 0x07060302u);
 }
 
-// Numerators of a lane's four tokens of two subtiles as pairs of halves; returns their sum.
-__device__ __forceinline__ float numerators(const f32x4_t& a, const f32x4_t& b, float scale_log2e, float neg_m, f16x8_t& p_hi, f16x8_t& p_lo) {
-  float sum = 0.f;
+// p - hi, where hi is the low (HIGH: high) half of a dword, in one instruction.
+template <bool HIGH>
+__device__ __forceinline__ float remainder_of(float p, f16x2_t hi) {
+  float r;
+  const uint32_t bits = __builtin_bit_cast(uint32_t, hi);
+  if constexpr (HIGH)
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(bits), "v"(p));
+  else
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(bits), "v"(p));
+  return r;
+}
+
+// Numerators of a lane's four tokens of two subtiles as pairs of halves.
+__device__ __forceinline__ void numerators(const f32x4_t& a, const f32x4_t& b, float scale_log2e, float neg_m, f16x8_t& p_hi, f16x8_t& p_lo) {
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const f32x4_t& s = e < 4 ? a : b;
     const f32x2_t p = {__builtin_amdgcn_exp2f(fmaf(s[e & 3], scale_log2e, neg_m)), __builtin_amdgcn_exp2f(fmaf(s[(e & 3) + 1], scale_log2e, neg_m))};
-    sum += p[0] + p[1];
     const f16x2_t hi = __builtin_convertvector(p, f16x2_t);
-    const f32x2_t rest = {p[0] - (float)hi[0], p[1] - (float)hi[1]};
+    const f32x2_t rest = {remainder_of<false>(p[0], hi), remainder_of<true>(p[1], hi)};
     const f16x2_t lo = __builtin_convertvector(rest, f16x2_t);
     p_hi[e] = hi[0];
     p_hi[e + 1] = hi[1];
     p_lo[e] = lo[0];
     p_lo[e + 1] = lo[1];
   }
-  return sum;
+}
+// One more row of values, all ones: its products with the numerators are their sums, on the matrix core, which has time for them where the vector
+// units have not.
+__device__ __forceinline__ f16x8_t ones() {
+  f16x8_t x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (_Float16)1.0f;
+  return x;
+}
+__device__ __forceinline__ f32x4_t sum_of(const f16x8_t& p_hi, const f16x8_t& p_lo, f32x4_t l) {
+  l = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones(), p_hi, l, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(ones(), p_lo, l, 0, 0, 0);
 }
 
 // ---- who does what.  The tiles of all (sequence, KV head) lists, one list behind the other and weighted with what a tile of so many query rows costs, are
@@ -121,13 +160,22 @@ __device__ __forceinline__ float numerators(const f32x4_t& a, const f32x4_t& b, 
 // heads, list h at [start, start + tiles * unit).  Tile t is workgroup (start + t * unit) / share's.  The partial of workgroup w for list h is item w + h.
 // Beyond kPlannedHeads lists every one has a workgroup of its own.
 struct Segment {
-  int b, j, head, M;       // M: query rows
-  int pages, t0, t1;       // listed pages, and the tiles [t0, t1) of them that are this workgroup's
-  int item;                // partial; negative: the list is finished here
+  int b, j, head, M;               // M: query rows
+  int base, tokens, seq_pages;     // the sequence
+  int pages, t0, t1;               // listed pages, and the tiles [t0, t1) of them that are this workgroup's
+  int item;                        // partial; negative: the list is finished here
 };
 __device__ __forceinline__ int row_blocks(int M, int most) { return (M + most - 1) / most; }
 // What a tile costs: converting it once per block of rows, and every 16 rows about as much as half of that.
 __device__ __forceinline__ int unit_cost(int M, int block) { return M <= 0 ? 0 : 2 * row_blocks(M, block) + row_blocks(M, 16); }
+
+// a / b for 0 <= a < 2^31 and a quotient below 2^20: the float's is off by one at most.
+__device__ __forceinline__ int quotient(int a, int b) {
+  int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+  const int r = a - q * b;
+  q += r >= b ? 1 : 0;
+  return q - (r < 0 ? 1 : 0);
+}
 
 // BLOCK: query rows that convert a tile once.  f(segment) for every list of this workgroup, in order.
 template <int GP, int BLOCK, typename F>
@@ -135,71 +183,75 @@ __device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& 
                                                  int workgroups, int least_tiles, int* plan, F f) {
   constexpr int PPT = 32 / GP;
   const int lane = threadIdx.x & 63;
-  auto list_of = [&](int h, int& M, int& pages) {
-    const int b = h / sh.Hkv;
-    M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
-    const Sequence seq = sequence_of(kv, sh, b);
-    pages = in.list ? max(0, min(min(in.sel_count[h], in.cap), sh.max_pages)) : seq.pages;
-  };
   if (workgroups == 0) {   // a list each
     Segment s;
     s.head = blockIdx.x;
     s.b = s.head / sh.Hkv;
     s.j = s.head % sh.Hkv;
-    list_of(s.head, s.M, s.pages);
+    s.M = min(active_rows(in, kv, sh, s.b), min(sh.rows_max, part.rows));
+    const Sequence seq = sequence(kv, sh, s.b);
+    s.base = seq.base;
+    s.tokens = seq.tokens;
+    s.seq_pages = seq.pages;
+    s.pages = in.list ? max(0, min(min(in.sel_count[s.head], in.cap), sh.max_pages)) : seq.pages;
     s.t0 = 0;
     s.t1 = (s.pages + PPT - 1) / PPT;
     s.item = -1;
     if (s.M > 0) f(s);
     return;
   }
-  // the plan, [start | tiles | unit | pages] per head in LDS: every wavefront makes it, all of them the same
+  // the plan in LDS, two int4 per head: every wavefront makes it, all of them the same
+  int4* const heads_plan = reinterpret_cast<int4*>(plan);
   int total = 0, most_unit = 1;
   for (int h0 = 0; h0 < heads; h0 += 64) {
-    const int h = h0 + lane;
-    int M = 0, pages = 0;
-    if (h < heads) list_of(h, M, pages);
+    const int h = min(h0 + lane, heads - 1), b = h / sh.Hkv;
+    int n = (in.active_count ? in.active_count : kv.seq_lens)[b], listed = *(in.list ? in.sel_count + h : kv.seq_lens + b);
+    const Sequence seq = sequence_of(kv, sh, b);
+    n = (in.active_count ? min(n, sh.B) : sh.B) * sh.G;
+    const int M = h0 + lane < heads ? min(n, min(sh.rows_max, part.rows)) : 0, pages = in.list ? max(0, min(min(listed, in.cap), sh.max_pages)) : seq.pages;
     const int unit = unit_cost(M, BLOCK), tiles = M > 0 ? (pages + PPT - 1) / PPT : 0, cost = tiles * unit;
     const int incl = wave_inclusive_scan(cost);
-    if (h < heads) reinterpret_cast<int4*>(plan)[h] = make_int4(total + incl - cost, tiles, unit, pages);
+    if (h0 + lane < heads) {
+      heads_plan[2 * h] = make_int4(total + incl - cost, tiles, unit, pages);
+      heads_plan[2 * h + 1] = make_int4(M, seq.base, seq.tokens, seq.pages);
+    }
     total += __builtin_amdgcn_readlane(incl, 63);
     most_unit = max(most_unit, (int)wave_max_u32((uint32_t)unit));
   }
   wave_lds_fence();
-  const int w = blockIdx.x, share = max((total + workgroups - 1) / workgroups, least_tiles * most_unit);
-  if (w == 0) {
-    for (int h = threadIdx.x; h < heads; h += blockDim.x) {
-      const int4 p = reinterpret_cast<const int4*>(plan)[h];
-      const int first = p.x / share, last = (p.x + (p.y - 1) * p.z) / share;
-      out.table[h] = make_int2(first + h, p.y > 0 ? last - first + 1 : 0);
-    }
-  }
+  const int w = blockIdx.x, share = max((int)((float)total / (float)workgroups * 1.000001f) + 1, least_tiles * most_unit);   // (at least total / workgroups)
   const int begin = w * share, end = begin + share;
-  int first = heads;
-  for (int h0 = 0; h0 < heads; h0 += 64) {   // the first list that reaches into the share
+  int first = heads, last = -1;   // the lists that reach into the share
+  for (int h0 = 0; h0 < heads; h0 += 64) {
     const int h = h0 + lane;
-    const int4 p = reinterpret_cast<const int4*>(plan)[min(h, heads - 1)];
-    const unsigned long long in_it = __ballot(h < heads && p.y > 0 && p.x + p.y * p.z > begin);
+    const int4 p = heads_plan[2 * min(h, heads - 1)];
+    const unsigned long long in_it = __ballot(h < heads && p.x < end && p.x + p.y * p.z > begin);
     if (in_it) {
-      first = h0 + __builtin_ctzll(in_it);
-      break;
+      first = min(first, h0 + __builtin_ctzll(in_it));
+      last = h0 + 63 - __builtin_clzll(in_it);
+    }
+    if (w == 0 && threadIdx.x < 64 && h < heads) {
+      const int from = quotient(p.x, share);
+      out.table[h] = make_int2(from + h, p.y > 0 ? quotient(p.x + (p.y - 1) * p.z, share) - from + 1 : 0);
     }
   }
-  for (int h = first; h < heads; ++h) {
-    const int4 p = reinterpret_cast<const int4*>(plan)[h];
+  for (int h = first; h <= last; ++h) {
+    const int4 p = heads_plan[2 * h], more = heads_plan[2 * h + 1];
     const int start = __builtin_amdgcn_readfirstlane(p.x), tiles = __builtin_amdgcn_readfirstlane(p.y), unit = __builtin_amdgcn_readfirstlane(p.z);
-    if (start >= end) break;
     if (tiles == 0) continue;
-    Segment s;
-    s.t0 = begin <= start ? 0 : (begin - start + unit - 1) / unit;
-    s.t1 = min(tiles, (end - start + unit - 1) / unit);
-    if (s.t0 >= s.t1) continue;
-    s.head = h;
-    s.b = h / sh.Hkv;
-    s.j = h - s.b * sh.Hkv;
-    s.M = min(active_rows(in, kv, sh, s.b), min(sh.rows_max, part.rows));
+    Segment s;   // (uniform, as the compiler does not see by itself)
+    s.head = __builtin_amdgcn_readfirstlane(h);
+    s.b = __builtin_amdgcn_readfirstlane(s.head / sh.Hkv);
+    s.j = __builtin_amdgcn_readfirstlane(s.head - s.b * sh.Hkv);
     s.pages = __builtin_amdgcn_readfirstlane(p.w);
-    s.item = s.t0 == 0 && s.t1 == tiles ? -1 : w + h;
+    s.M = __builtin_amdgcn_readfirstlane(more.x);
+    s.base = __builtin_amdgcn_readfirstlane(more.y);
+    s.tokens = __builtin_amdgcn_readfirstlane(more.z);
+    s.seq_pages = __builtin_amdgcn_readfirstlane(more.w);
+    s.t0 = begin <= start ? 0 : __builtin_amdgcn_readfirstlane(quotient(begin - start + unit - 1, unit));
+    s.t1 = min(tiles, __builtin_amdgcn_readfirstlane(quotient(end - start + unit - 1, unit)));
+    if (s.t0 >= s.t1) continue;
+    s.item = s.t0 == 0 && s.t1 == tiles ? -1 : w + s.head;
     f(s);
   }
 }
@@ -225,160 +277,212 @@ __device__ __forceinline__ void store_state(const Shape& sh, const AttnInputs& i
   if (channel == 0) out.lse_p[orow] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup of up to 64 rows does.  Its WAVES wavefronts deal the share's tiles out, two
+// Sixteen bytes a lane from `base` + offset to LDS at `to` + 16 lane, without a register on the way.  The wavefront waits for them itself (landed()).
+// (In assembly, as the compiler waits for all of them ahead of any LDS read; there is no output that it could take for written.  It keeps nothing
+// in M0 from one instruction to another.)
+__device__ __forceinline__ void start_to_lds(const uint8_t* base, uint32_t offset, uint32_t to) {
+  const uint64_t at = (uint64_t)(uintptr_t)base;
+  const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(uniform), "s"(to) : "memory");
+}
+// ... from an address of each lane's own: two pages are any distance apart, in either direction, and an offset is 32 bits without a sign.
+__device__ __forceinline__ void start_to_lds(const uint8_t* lane_address, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(lane_address), "s"(to) : "memory");
+}
+// All but the last N of them are there.
+template <int N>
+__device__ __forceinline__ void landed() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup of up to 64 rows does.  Its wavefronts deal the share's tiles out, two
 // wavefronts to a SIMD, so that one's matrix products run beside the other's vector work.  That takes 256 registers a lane at most:
-//   a tile's codes have no second buffer: the next tile's keys are requested when this one's have been converted, its values after
-//     the last product (what is on its way per compute unit is still some 24 KiB);
+//   tiles come into LDS, a ring of kRing per wavefront, all but one of them on their way (70 KiB per compute unit);
 //   the query fragments are read from LDS for every tile where there are more than two row tiles (or float queries).
 // Four row tiles do not fit.  They are two sets of two (SETS): a wavefront of each set takes every tile, which reads its codes from
 // the cache the second time and converts them twice, 128 of some 240 vector instructions a tile.
-constexpr int kSlots = 4;   // LDS images of a wavefront's state (of a set): half of the wavefronts hand theirs over, twice; with two sets all have one
+constexpr int kWaves = 8, kRing = 3;
 template <int R, int D, int NQ, int SETS = 1>
 struct DealtLds {
   static constexpr bool kQueries = R > 2 || NQ > 1;
   static constexpr int kState = R * (D / 16) * 256 + 2 * R * 16;                    // floats: O as [row tile][channel tile][lane] vectors, references, sums
   static constexpr int kQueryFloats = kQueries ? NQ * R * (D / 32) * 256 : 0;
-  static constexpr int kBytes = (kQueryFloats + SETS * kSlots * kState) * (int)sizeof(float);
+  static constexpr int kTile = 32 * D + 64 * (D / 32);                              // bytes of a tile: keys, values, scales
+  // LDS images of the wavefronts' states: all of them, or where there is no room for that half (each wavefront of the second half hands its state
+  // to one of the first, before those hand theirs to everybody)
+  static constexpr bool kAll = (kQueryFloats + kWaves * kState) * 4 + kPlannedHeads * 32 <= 160 * 1024;
+  static constexpr int kSlots = (kAll ? kWaves : kWaves / 2) / SETS;                // of a set
+  static constexpr int kRingBytes = kWaves * kRing * kTile, kStateBytes = SETS * kSlots * kState * 4;   // (one after the other in the same place)
+  static constexpr int kBytes = kQueryFloats * 4 + (kRingBytes > kStateBytes ? kRingBytes : kStateBytes);
 };
 template <int D, int GP, int R, int NQ, int SETS = 1>
 __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, const Segment& seg, int row_base,
                                                  const Partials& part, const PackedOut& out, float scale_log2e, float* lds) {
-  constexpr int WAVES = 2 * kSlots / SETS;   // of a set
-  constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32;   // products per score, channel tiles, groups, dwords a lane reads of a subtile
+  constexpr int WAVES = kWaves / SETS;   // of a set
+  constexpr int KS = D / 32, NT = D / 16, J = D / 32, W = D / 32;   // products per score, channel tiles, groups, dwords a lane has of a subtile
   constexpr int CPL = D / 4;                                        // channels of a token that a lane has
   constexpr int PPT = 32 / GP, TPR = 64 / PPT;                      // pages per tile, tiles per fetch of page entries
-  constexpr int kTileBytes = GP * D / 2;
+  constexpr int kPageBytes = GP * D / 2, kPageScales = 2 * GP * J;
   typedef DealtLds<R, D, NQ, SETS> Lds;
-  static_assert(SETS == 1 || !Lds::kQueries, "the sets' queries are not the same");
+  static_assert(SETS == 1 || (!Lds::kQueries && Lds::kAll), "the sets' queries are not the same, and a wavefront hands its state to one of its set");
   constexpr bool kTight = D == 128 && Lds::kQueries;   // registers are short
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));   // (what derives from it is worked out per segment, not kept in registers over all of them)
   const int in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_group % WAVES, set = in_group / WAVES;
   const int l16 = lane & 15, qd = lane >> 4;
   const int b = seg.b, j = seg.j, M = seg.M, row0 = row_base + set * (R * 16);
-  const Sequence seq = sequence(kv, sh, b);
   // tiles are dealt round-robin to the wavefronts
   const int tfirst = seg.t0 + wave, ntw = tfirst < seg.t1 ? (seg.t1 - 1 - tfirst) / WAVES + 1 : 0;
 
-  // ---- pages of this wavefront's next TPR tiles, one per lane
+  // ---- pages of this wavefront's next TPR tiles, one per lane: list entry, page table, decoded
   int pg_phys = 0, pg_valid = 0;
-  auto fetch_pages = [&](int n0) {
+  auto listed = [&](int n0) {
     const int at = (tfirst + (n0 + lane / PPT) * WAVES) * PPT + lane % PPT;
-    int logical = -1, phys = -1;
-    if (at < seg.pages) logical = in.list ? in.list[(size_t)seg.head * in.cap + at] : at;
-    if ((unsigned)logical < (unsigned)seq.pages) phys = kv.page_indices[seq.base + logical];
+    int logical = at < seg.pages ? at : -1;
+    if (in.list && at < seg.pages) logical = in.list[(size_t)seg.head * in.cap + at];
+    return logical;
+  };
+  auto entry = [&](int logical) { return (unsigned)logical < (unsigned)seg.seq_pages ? kv.page_indices[seg.base + logical] : -1; };
+  auto decode = [&](int logical, int phys) {
     const bool ok = (unsigned)phys < (unsigned)kv.num_pages;
     pg_phys = ok ? phys : 0;
-    pg_valid = ok ? min(GP, seq.tokens - logical * GP) : 0;
+    pg_valid = ok ? min(GP, seg.tokens - logical * GP) : 0;
   };
-  struct Keys {
-    uint32_t c[2][W], s[2];
-  } k;
-  struct Values {
-    uint32_t c[2][W], s[2][4];   // s: scales of the lane's four tokens, a byte per group
-  } v;
-  int nv[2] = {0, 0}, nv_next[2] = {0, 0};   // valid tokens of the two subtiles
-  // tile n (where there is none, the pool's first page: nothing is made of it)
-  auto page_of = [&](int n, int s) {
-    const int at = GP == 16 ? (2 * n + s) & 63 : n & 63;
-    return n < ntw ? __builtin_amdgcn_readlane(pg_phys, at) : 0;
-  };
-  auto load_keys = [&](int n) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const size_t tile = (size_t)page_of(n, s) * sh.Hkv + j;
-      const int row = (GP == 16 ? 0 : 16 * s) + l16;
-      load_dwords<W>(pk.k + tile * kTileBytes + row * (D / 2) + qd * (CPL / 2), k.c[s]);
-      k.s[s] = pk.scales[tile * (2 * GP * J) + row * J + qd * CPL / 32];
-      nv_next[s] = __builtin_amdgcn_readlane(pg_valid, GP == 16 ? (2 * n + s) & 63 : n & 63) - (GP == 16 ? 0 : 16 * s);
-    }
-  };
-  auto load_values = [&](int n) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const size_t tile = (size_t)page_of(n, s) * sh.Hkv + j;
-      const int quad = (GP == 16 ? 0 : 4 * s) + qd;
-      load_dwords<W>(pk.v + tile * kTileBytes + (quad * 16 + l16) * (J * 4), v.c[s]);
-      load_scales<J>(pk.scales + tile * (2 * GP * J) + GP * J + quad * 4 * J, v.s[s]);
-    }
-  };
-  fetch_pages(0);
-  load_keys(0);
-  load_values(0);
 
-  // ---- query rows, in the order the keys' channels are contracted in: fragment (row tile, term, product)
-  bf16x8_t qf[Lds::kQueries ? 1 : R][NQ][KS];
-  auto query = [&](int mt, int ks, bf16x8_t (&term)[NQ]) {
-    const int r = row0 + mt * 16 + l16, rr = min(r, sh.rows_max - 1), a = row_token(sh, rr);
-    const int tok = in.active_idx ? in.active_idx[(size_t)b * sh.B + a] : a;
-    const bool keep = r < M && (unsigned)tok < (unsigned)sh.B;
-    const size_t at = (((size_t)b * sh.B + (keep ? tok : 0)) * sh.Hq + j * sh.G + (rr - a * sh.G)) * D + qd * CPL + ks * 8;
+  // ---- the way to the first tile: list entries and the query rows' tokens, then page table and query rows, each pair in one memory round trip
+  constexpr int kFragments = R * KS, kOwn = Lds::kQueries ? (kFragments + WAVES - 1) / WAVES : kFragments;   // of queries; that this wavefront fetches
+  const int logical = listed(0);
+  int tok[Lds::kQueries ? kOwn : R];
+#pragma unroll
+  for (int i = 0; i < (Lds::kQueries ? kOwn : R); ++i) {
+    const int mt = Lds::kQueries ? (wave + i * WAVES) / KS : i, a = row_token(sh, min(row0 + mt * 16 + l16, sh.rows_max - 1));
+    tok[i] = in.active_idx ? in.active_idx[(size_t)b * sh.B + a] : a;
+  }
+  const int phys = entry(logical);
+  uint4 q_raw[kOwn][NQ == 1 ? 1 : 2];
+  bool q_keep[kOwn];
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int f = Lds::kQueries ? wave + i * WAVES : i, mt = f / KS, ks = f % KS, t = tok[Lds::kQueries ? i : mt];
+    const int r = row0 + mt * 16 + l16, rr = min(r, sh.rows_max - 1);
+    q_keep[i] = r < M && (unsigned)t < (unsigned)sh.B;
+    const size_t at = (((size_t)b * sh.B + (q_keep[i] ? t : 0)) * sh.Hq + j * sh.G + (rr - row_token(sh, rr) * sh.G)) * D + qd * CPL + ks * 8;
     if constexpr (NQ == 1) {
-      uint4 x = *reinterpret_cast<const uint4*>((const bf16_t*)in.q + at);
-      if (!keep) x = make_uint4(0u, 0u, 0u, 0u);
-      term[0] = __builtin_bit_cast(bf16x8_t, x);
+      q_raw[i][0] = *reinterpret_cast<const uint4*>((const bf16_t*)in.q + at);
     } else {
-      float x[8];
-      load_floats8((const float*)in.q + at, x);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (!keep) x[e] = 0.f;
-          const __bf16 t = (__bf16)x[e];
-          term[n][e] = t;
-          x[e] -= (float)t;
-        }
+      q_raw[i][0] = *reinterpret_cast<const uint4*>((const float*)in.q + at);
+      q_raw[i][1] = *reinterpret_cast<const uint4*>((const float*)in.q + at + 4);
     }
+  }
+  decode(logical, phys);
+
+  // ---- the ring: keys of subtiles 0 and 1, values of both, scales as they lie
+  constexpr int kLoads = D == 128 ? 5 : 3;   // loads per tile
+  char* const ring = reinterpret_cast<char*>(lds + Lds::kQueryFloats) + in_group * (kRing * Lds::kTile);
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+  int nv[kRing][2];   // valid tokens of the subtiles of the tiles n, n + 1, ... (the first kRing - 1 of them before tile n + kRing - 1 is started)
+  auto start_tile = [&](int n, int slot) {
+    const int e0 = GP == 16 ? (2 * n) & 63 : n & 63, e1 = GP == 16 ? e0 + 1 : e0;
+    int p0 = __builtin_amdgcn_readlane(pg_phys, e0), p1 = __builtin_amdgcn_readlane(pg_phys, e1);
+    nv[kRing - 1][0] = __builtin_amdgcn_readlane(pg_valid, e0);
+    nv[kRing - 1][1] = GP == 16 ? __builtin_amdgcn_readlane(pg_valid, e1) : nv[kRing - 1][0] - 16;
+    // (a tile that does not exist: the pool's first page, so that the loads on their way are the same number always)
+    p0 = n < ntw ? p0 : 0;
+    p1 = n < ntw ? p1 : 0;
+    const size_t t0 = (size_t)p0 * sh.Hkv + j, t1 = (size_t)p1 * sh.Hkv + j;
+    const uint32_t to = ring_at + slot * Lds::kTile;
+    if constexpr (D == 128) {
+      const uint32_t key = l16 * 64 + qd * 16, value = lane * 16, second = GP == 16 ? 0 : 1024;
+      start_to_lds(pk.k + t0 * kPageBytes, key, to);
+      start_to_lds(pk.k + t1 * kPageBytes + second, key, to + 1024);
+      start_to_lds(pk.v + t0 * kPageBytes, value, to + 2048);
+      start_to_lds(pk.v + t1 * kPageBytes + second, value, to + 3072);
+    } else {
+      // two pages' 512 bytes are a load: lanes 32 .. 63 have the second's
+      const size_t from = GP == 16 ? (lane < 32 ? t0 : t1) * kPageBytes + (lane & 31) * 16 : t0 * kPageBytes + lane * 16;
+      start_to_lds(pk.k + from, to);
+      start_to_lds(pk.v + from, to + 1024);
+    }
+    constexpr int kPieces = kPageScales / 16;   // of a page
+    if (lane < kPieces * PPT)
+      start_to_lds(pk.scales + (lane < kPieces ? t0 : t1) * kPageScales + lane % kPieces * 16, to + 32 * D);
   };
-  const bf16x8_t* const q_lds = reinterpret_cast<const bf16x8_t*>(lds);
-  if constexpr (Lds::kQueries) {
-    for (int f = wave; f < R * KS; f += WAVES) {
-      bf16x8_t term[NQ];
-      query(f / KS, f % KS, term);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) reinterpret_cast<bf16x8_t*>(lds)[(f * NQ + n) * 64 + lane] = term[n];
-    }
-    __syncthreads();
-  } else {
-#pragma unroll
-    for (int mt = 0; mt < R; ++mt)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        bf16x8_t term[NQ];
-        query(mt, ks, term);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) qf[mt][n][ks] = term[n];
-      }
+  for (int n = 0; n < kRing - 1; ++n) {
+    start_tile(n, n);
+    nv[n][0] = nv[kRing - 1][0];
+    nv[n][1] = nv[kRing - 1][1];
   }
 
-  float m_run[R], l_run[R], up_thr[R];
+  // ---- query rows, in the order the keys' channels are contracted in: fragment (row tile, product), its terms
+  bf16x8_t qf[Lds::kQueries ? 1 : R][NQ][KS];
+  const bf16x8_t* const q_lds = reinterpret_cast<const bf16x8_t*>(lds);
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    bf16x8_t term[NQ];
+    if constexpr (NQ == 1) {
+      uint4 x = q_raw[i][0];
+      if (!q_keep[i]) x = make_uint4(0u, 0u, 0u, 0u);
+      term[0] = __builtin_bit_cast(bf16x8_t, x);
+    } else {
+      const uint4 lo = q_raw[i][0], hi = q_raw[i][1];
+      const uint32_t bits[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float x = q_keep[i] ? __uint_as_float(bits[e]) : 0.f;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          term[n][e] = (__bf16)x;
+          x -= (float)term[n][e];
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      if constexpr (Lds::kQueries) {
+        const int f = wave + i * WAVES;
+        if (f < kFragments) reinterpret_cast<bf16x8_t*>(lds)[(f * NQ + n) * 64 + lane] = term[n];
+      } else {
+        qf[i / KS][n][i % KS] = term[n];
+      }
+    }
+  }
+  if constexpr (Lds::kQueries) __syncthreads();
+
+  float m_run[R], up_thr[R];
   const float inv_scale_log2e = 1.0f / scale_log2e;
-  f32x4_t o[R][NT];
+  f32x4_t o[R][NT], l_sum[R];   // (a row's sum in all four components)
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) {
     m_run[mt] = kNegBig;
     up_thr[mt] = -INFINITY;
-    l_run[mt] = 0.f;
+    l_sum[mt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) o[mt][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   }
 
+  int slot_now = 0, slot_next = kRing - 1;
   for (int n = 0; n < ntw; ++n) {
-    nv[0] = nv_next[0];
-    nv[1] = nv_next[1];
-    if ((n + 1) % TPR == 0) fetch_pages(n + 1);   // (the entries are decoded behind the branch, so nothing waits where it joins)
+    if ((n + kRing - 1) % TPR == 0) {   // (the entries are decoded behind the branch, so nothing waits where it joins)
+      const int next = listed(n + kRing - 1);
+      decode(next, entry(next));
+    }
+    start_tile(n + kRing - 1, slot_next);
+    landed<kLoads * (kRing - 1)>();
+    const char* tile = ring + slot_now * Lds::kTile;
+    const uint8_t* scales = reinterpret_cast<const uint8_t*>(tile + 32 * D);
     // scores, a subtile at a time (the barriers keep what is read or converted ahead, and so the registers, to that)
     f32x4_t sc[R][2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const float scale = power_of(k.s[s]);
+      uint32_t c[W];
+      lds_dwords<W>(tile + (D == 128 ? s * 1024 + lane * 16 : s * 512 + l16 * 32 + qd * 8), c);
+      const float scale = power_of(scales[(GP == 16 ? s * kPageScales + l16 * J : (16 * s + l16) * J) + qd * CPL / 32]);
       bf16x8_t kf[KS];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        kf[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(codes_to_bf16<0>(k.c[s][ks], scale), codes_to_bf16<1>(k.c[s][ks], scale),
-                                                         codes_to_bf16<2>(k.c[s][ks], scale), codes_to_bf16<3>(k.c[s][ks], scale)));
-      if (s == 1) load_keys(n + 1);
+        kf[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(codes_to_bf16<0>(c[ks], scale), codes_to_bf16<1>(c[ks], scale),
+                                                         codes_to_bf16<2>(c[ks], scale), codes_to_bf16<3>(c[ks], scale)));
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) {
         sc[mt][s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
@@ -396,13 +500,19 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
       }
       if constexpr (kTight) __builtin_amdgcn_sched_barrier(0);
     }
-    if (!(nv[0] >= 16 && nv[1] >= 16)) {   // slots behind the sequence's end may hold anything
+    uint32_t vc[2][W], vs[2][4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      lds_dwords<W>(tile + 16 * D + (D == 128 ? s * 1024 + lane * 16 : s * 512 + lane * 8), vc[s]);
+      load_scales<J>(scales + (GP == 16 ? s * kPageScales + GP * J + qd * 4 * J : GP * J + (16 * s + qd * 4) * J), vs[s]);
+    }
+    if (!(nv[0][0] >= 16 && nv[0][1] >= 16)) {   // slots behind the sequence's end may hold anything
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const bool there = qd * 4 + e < nv[s];
-          v.s[s][e] = there ? v.s[s][e] : 0u;   // (the smallest scale: nothing, in half precision)
+          const bool there = qd * 4 + e < nv[0][s];
+          vs[s][e] = there ? vs[s][e] : 0u;   // (the smallest scale: nothing, in half precision)
 #pragma unroll
           for (int mt = 0; mt < R; ++mt) sc[mt][s][e] = there ? sc[mt][s][e] : -INFINITY;
         }
@@ -424,7 +534,7 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
         const float alpha = up ? __builtin_amdgcn_exp2f(m_run[mt] - cand) : 1.0f;
         m_run[mt] = up ? cand : m_run[mt];
         up_thr[mt] = (m_run[mt] + kHeadroom + kLag) * inv_scale_log2e;
-        l_run[mt] *= alpha;
+        l_sum[mt] *= alpha;
         if (n > 0) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) o[mt][nt] *= alpha;
@@ -433,15 +543,17 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
     }
     f16x8_t p_hi[R], p_lo[R];
 #pragma unroll
-    for (int mt = 0; mt < R; ++mt) l_run[mt] += numerators(sc[mt][0], sc[mt][1], scale_log2e, -m_run[mt], p_hi[mt], p_lo[mt]);
+    for (int mt = 0; mt < R; ++mt) {
+      numerators(sc[mt][0], sc[mt][1], scale_log2e, -m_run[mt], p_hi[mt], p_lo[mt]);
+      l_sum[mt] = sum_of(p_hi[mt], p_lo[mt], l_sum[mt]);
+    }
 #pragma unroll
     for (int g = 0; g < J; ++g) {
       uint2 lo[2], hi[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) value_operands(v.c[s][g], v.s[s], g, lo[s], hi[s]);
+      for (int s = 0; s < 2; ++s) value_operands(vc[s][g], vs[s], g, lo[s], hi[s]);
       const f16x8_t va = __builtin_bit_cast(f16x8_t, make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y));
       const f16x8_t vb = __builtin_bit_cast(f16x8_t, make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y));
-      if (g == J - 1) load_values(n + 1);
       if constexpr (kTight) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) {
@@ -454,14 +566,24 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
         o[mt][2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, p_lo[mt], o[mt][2 * g + 1], 0, 0, 0);
       }
     }
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) {
+      nv[i][0] = nv[i + 1][0];
+      nv[i][1] = nv[i + 1][1];
+    }
+    slot_now = slot_now == kRing - 1 ? 0 : slot_now + 1;
+    slot_next = slot_next == kRing - 1 ? 0 : slot_next + 1;
   }
 
-  // ---- the wavefronts' states become one partial, in a fixed order: the second half of them hands its states to the first through LDS, those hand theirs
-  // to everybody, and each wavefront makes some of the partial's vectors
+  // ---- the wavefronts' states become one partial, in a fixed order, each wavefront making some of its vectors
+  landed<0>();
+  __syncthreads();   // the rings' place is the states' now
+  float l_run[R];
 #pragma unroll
-  for (int mt = 0; mt < R; ++mt) l_run[mt] = over_lane_groups_sum(l_run[mt]);
+  for (int mt = 0; mt < R; ++mt) l_run[mt] = l_sum[mt][0];
   float* const states = lds + Lds::kQueryFloats;
-  float* const slot = states + (SETS == 1 ? wave % kSlots : in_group) * Lds::kState;
+  constexpr int kSlots = Lds::kSlots;
+  float* const slot = states + (Lds::kAll ? in_group : wave % kSlots) * Lds::kState;
   auto publish = [&]() {
 #pragma unroll
     for (int mt = 0; mt < R; ++mt) {
@@ -473,7 +595,7 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
       for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4_t*>(slot + ((mt * NT + nt) * 64 + lane) * 4) = o[mt][nt];
     }
   };
-  if constexpr (SETS == 1) {
+  if constexpr (!Lds::kAll) {
     if (wave >= kSlots) publish();
     __syncthreads();
     if (wave < kSlots) {
@@ -537,7 +659,6 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, qd = lane >> 4;
   const int b = seg.b, j = seg.j, M = seg.M, row0 = row_base + wave * (R * 16);
-  const Sequence seq = sequence(kv, sh, b);
   const int stages = (seg.t1 - seg.t0 + 1) / 2;
 
   bf16x8_t qf[R][KS];
@@ -561,10 +682,10 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     const int tile = seg.t0 + n0 + lane / PPT, at = tile * PPT + lane % PPT;
     int logical = -1, phys = -1;
     if (tile < seg.t1 && at < seg.pages) logical = in.list ? in.list[(size_t)seg.head * in.cap + at] : at;
-    if ((unsigned)logical < (unsigned)seq.pages) phys = kv.page_indices[seq.base + logical];
+    if ((unsigned)logical < (unsigned)seg.seq_pages) phys = kv.page_indices[seg.base + logical];
     const bool ok = (unsigned)phys < (unsigned)kv.num_pages;
     pg_phys = ok ? phys : 0;
-    pg_valid = ok ? min(GP, seq.tokens - logical * GP) : 0;
+    pg_valid = ok ? min(GP, seg.tokens - logical * GP) : 0;
   };
   // valid tokens of subtile s of stage i (of the TPR tiles at hand)
   auto valid_of = [&](int i, int s) {
@@ -611,14 +732,14 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     }
   };
 
-  float m_run[R], l_run[R], up_thr[R];
+  float m_run[R], up_thr[R];
   const float inv_scale_log2e = 1.0f / scale_log2e;
-  f32x4_t o[R][NT];
+  f32x4_t o[R][NT], l_sum[R];   // (a row's sum in all four components)
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) {
     m_run[mt] = kNegBig;
     up_thr[mt] = -INFINITY;
-    l_run[mt] = 0.f;
+    l_sum[mt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) o[mt][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   }
@@ -667,7 +788,7 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
         const float alpha = up ? __builtin_amdgcn_exp2f(m_run[mt] - cand) : 1.0f;
         m_run[mt] = up ? cand : m_run[mt];
         up_thr[mt] = (m_run[mt] + kHeadroom + kLag) * inv_scale_log2e;
-        l_run[mt] *= alpha;
+        l_sum[mt] *= alpha;
         if (!first) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) o[mt][nt] *= alpha;
@@ -678,7 +799,10 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     for (int h = 0; h < 2; ++h) {   // a pair of subtiles at a time
       f16x8_t p_hi[R], p_lo[R];
 #pragma unroll
-      for (int mt = 0; mt < R; ++mt) l_run[mt] += numerators(sc[mt][2 * h], sc[mt][2 * h + 1], scale_log2e, -m_run[mt], p_hi[mt], p_lo[mt]);
+      for (int mt = 0; mt < R; ++mt) {
+        numerators(sc[mt][2 * h], sc[mt][2 * h + 1], scale_log2e, -m_run[mt], p_hi[mt], p_lo[mt]);
+        l_sum[mt] = sum_of(p_hi[mt], p_lo[mt], l_sum[mt]);
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const f16x8_t vf = *reinterpret_cast<const f16x8_t*>(buf + 64 * D * 2 + ((h * NT + nt) * 64 + lane) * 16);
@@ -714,22 +838,19 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     }
   }
 
-  float l_row[R];
-#pragma unroll
-  for (int mt = 0; mt < R; ++mt) l_row[mt] = over_lane_groups_sum(l_run[mt]);
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) {
     const int r = row0 + mt * 16 + l16;
     if (r >= M) continue;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) store_state<D>(sh, in, part, out, seg, r, nt * 16 + qd * 4, o[mt][nt], m_run[mt], l_row[mt]);
+    for (int nt = 0; nt < NT; ++nt) store_state<D>(sh, in, part, out, seg, r, nt * 16 + qd * 4, o[mt][nt], m_run[mt], l_sum[mt][0]);
   }
 }
 
 #define LOSA_PACKED_ARGS KvView kv, Shape sh, AttnInputs in, PackedView pk, Partials part, PackedOut out, float scale_log2e, int heads, int workgroups, int least_tiles
 // Rows that the host knows: blocks of SETS * R row tiles, one after the other.
 template <int D, int GP, int R, int NQ, int SETS = 1>
-__global__ __launch_bounds__(128 * kSlots) void packed_attn_kernel(LOSA_PACKED_ARGS) {
+__global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   constexpr int kRows = SETS * R * 16;
   int* plan = reinterpret_cast<int*>(lds) + DealtLds<R, D, NQ, SETS>::kBytes / 4;
@@ -753,7 +874,7 @@ constexpr int kCountedRows = NQ == 1 ? 64 : 32;
 template <int D, int NQ>
 constexpr int kCountedBytes = NQ == 1 ? std::max(DealtLds<3, D, 1>::kBytes, DealtLds<2, D, 1, 2>::kBytes) : DealtLds<2, D, NQ>::kBytes;
 template <int D, int GP, int NQ>
-__global__ __launch_bounds__(128 * kSlots) void packed_attn_counted_kernel(LOSA_PACKED_ARGS) {
+__global__ __launch_bounds__(64 * kWaves) void packed_attn_counted_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   int* plan = reinterpret_cast<int*>(lds) + kCountedBytes<D, NQ> / 4;
   for_each_segment<GP, kCountedRows<NQ>>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
@@ -846,9 +967,9 @@ template <int D, int GP>
 static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int heads, int workgroups,
                             int least_tiles, int rows, bool known, const Partials& part, const PackedOut& out) {
   auto go = [&](PackedKernel kern, int lds_bytes, bool& attr_set) {
-    const int all = lds_bytes + (workgroups ? heads * 16 : 0);   // the plan behind the kernel's own
+    const int all = lds_bytes + (workgroups ? heads * 32 : 0);   // the plan behind the kernel's own
     if (!attr_set) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes + kPlannedHeads * 16);
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes + kPlannedHeads * 32);
       if (e != hipSuccess) return e;
       attr_set = true;
     }
