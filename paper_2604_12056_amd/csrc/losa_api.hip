@@ -107,7 +107,7 @@ constexpr long kMergedShares = 64;        // shares of a row that the merge kern
 constexpr long kFewPartials = 4096;       // rows of partials in all that a launch may have for a share per two tiles
 constexpr long kFloatGroups = 2;          // float-mode workgroups per bfloat16 attention workgroup aimed at: two fit a CU
 constexpr long kScoreRound = 5L * 256;    // scoring workgroups counted as one round: four per CU are resident, a quarter more start as those end
-constexpr int kLeastTiles = 8;            // tiles of a share of the attention over a 4-bit cache: one for each wavefront
+constexpr int kLeastTiles = 4;            // tiles of a share of the attention over a 4-bit cache: one for each wavefront
 constexpr int kSparseRows = 64;           // query rows per KV head up to which the split-pages work shape is used
 
 thread_local char g_create_err[256] = "";
@@ -521,10 +521,19 @@ losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, co
   if (!known) rows_upper = ctx->sh.rows_max;
   Partials part = ctx->part;
   part.rows = known ? std::min((rows_upper + 15) / 16 * 16, ctx->sh.rows_max) : ctx->sh.rows_max;
-  // Shares of all lists, while there are partials for them; the union bitmaps, which nothing reads after the scoring, hold the table that says
-  // which partials a list has.
-  const long heads = (long)batch * ctx->sh.Hkv, room = ctx->part_rows / part.rows - heads;
-  const long workgroups = heads <= kPlannedHeads && room >= kTargetWorkgroups / 2 ? std::min(ctx->target_workgroups, room) : 0;
+  // Shares of all lists, while there are partials for them: two workgroups to a compute unit up to 64 rows, one beyond.  The partials lie where the
+  // scores are, which nothing reads any more, if there is more room; and the union bitmaps hold the table that says which partials a list has.
+  const long heads = (long)batch * ctx->sh.Hkv, d = ctx->sh.d;
+  long room = ctx->part_rows / part.rows;
+  const long in_scores = (long)ctx->cfg.max_batch * ctx->sh.Hkv * ctx->sh.rows_max * ctx->sh.max_pages / ((d + 2) * part.rows);
+  if (in_scores > room) {
+    room = in_scores;
+    part.o = ctx->scores;
+    part.m = part.o + room * part.rows * d;
+    part.l = part.m + room * part.rows;
+  }
+  const long target = ctx->target_workgroups * (known && rows_upper > kSparseRows && ctx->cfg.dtype == LOSA_BF16 ? 1 : 2);
+  const long workgroups = heads <= kPlannedHeads && room - heads >= kTargetWorkgroups / 2 ? std::min(target, room - heads) : 0;
   const AttnInputs in{q, active_idx, active_count, sel_pages, sel_count, cap};
   const PackedOut out{o_p, lse_p, (int2*)ctx->union_bits};
   hipError_t e;
@@ -535,7 +544,7 @@ losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, co
   if (e != hipSuccess) return hip_fail(ctx, "packed attention launch", e);
   if (workgroups == 0) return LOSA_OK;
   StageTimer timer(ctx, st, LOSA_STAGE_MERGE);
-  e = launch_packed_join(st, kv, ctx->sh, batch, in, rows_upper, known, part, out);
+  e = launch_packed_join(st, kv, ctx->sh, batch, in, (int)workgroups, rows_upper, known, part, out);
   if (e != hipSuccess) return hip_fail(ctx, "packed join launch", e);
   return LOSA_OK;
 }

@@ -266,8 +266,8 @@ struct PackedOut {
 };
 hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk, int workgroups,
                               int least_tiles, int rows, bool rows_known, const Partials& part, const PackedOut& out);
-hipError_t launch_packed_join(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, int rows, bool rows_known, const Partials& part,
-                              const PackedOut& out);
+hipError_t launch_packed_join(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, int workgroups, int rows, bool rows_known,
+                              const Partials& part, const PackedOut& out);
 
 // ---- block_merge.hip
 hipError_t launch_block_merge(hipStream_t st, int dtype, const Shape& sh, int batch, const void* q, const void* k_b,

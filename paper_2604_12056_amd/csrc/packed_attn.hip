@@ -204,7 +204,7 @@ __device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& 
   int4* const heads_plan = reinterpret_cast<int4*>(plan);
   int total = 0, most_unit = 1;
   for (int h0 = 0; h0 < heads; h0 += 64) {
-    const int h = min(h0 + lane, heads - 1), b = h / sh.Hkv;
+    const int h = min(h0 + lane, heads - 1), b = quotient(h, sh.Hkv);
     int n = (in.active_count ? in.active_count : kv.seq_lens)[b], listed = *(in.list ? in.sel_count + h : kv.seq_lens + b);
     const Sequence seq = sequence_of(kv, sh, b);
     n = (in.active_count ? min(n, sh.B) : sh.B) * sh.G;
@@ -219,7 +219,7 @@ __device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& 
     most_unit = max(most_unit, (int)wave_max_u32((uint32_t)unit));
   }
   wave_lds_fence();
-  const int w = blockIdx.x, share = max((int)((float)total / (float)workgroups * 1.000001f) + 1, least_tiles * most_unit);   // (at least total / workgroups)
+  const int w = blockIdx.x, share = max((int)((float)total * (1.000001f * __builtin_amdgcn_rcpf((float)workgroups))) + 1, least_tiles * most_unit);   // (at least total / workgroups)
   const int begin = w * share, end = begin + share;
   int first = heads, last = -1;   // the lists that reach into the share
   for (int h0 = 0; h0 < heads; h0 += 64) {
@@ -241,7 +241,7 @@ __device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& 
     if (tiles == 0) continue;
     Segment s;   // (uniform, as the compiler does not see by itself)
     s.head = __builtin_amdgcn_readfirstlane(h);
-    s.b = __builtin_amdgcn_readfirstlane(s.head / sh.Hkv);
+    s.b = __builtin_amdgcn_readfirstlane(quotient(h, sh.Hkv));
     s.j = __builtin_amdgcn_readfirstlane(s.head - s.b * sh.Hkv);
     s.pages = __builtin_amdgcn_readfirstlane(p.w);
     s.M = __builtin_amdgcn_readfirstlane(more.x);
@@ -295,22 +295,26 @@ __device__ __forceinline__ void landed() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup of up to 64 rows does.  Its wavefronts deal the share's tiles out, two
-// wavefronts to a SIMD, so that one's matrix products run beside the other's vector work.  That takes 256 registers a lane at most:
-//   tiles come into LDS, a ring of kRing per wavefront, all but one of them on their way (70 KiB per compute unit);
+// Query rows row0 .. row0 + 16 R - 1 of a (sequence, KV head): what a workgroup of up to 64 rows does.  Its four wavefronts deal the share's tiles out.  Two
+// workgroups fit a compute unit, so that one's way to its first tile and the joining of its wavefronts' states, some 10 us together, run beside the
+// other's tiles.  That takes 256 registers a lane and 80 KiB of LDS at most:
+//   tiles come into LDS, a ring of kRing per wavefront, all but two of them on their way;
 //   the query fragments are read from LDS for every tile where there are more than two row tiles (or float queries).
 // Four row tiles do not fit.  They are two sets of two (SETS): a wavefront of each set takes every tile, which reads its codes from
 // the cache the second time and converts them twice, 128 of some 240 vector instructions a tile.
-constexpr int kWaves = 8, kRing = 3;
+constexpr int kWaves = 4;
 template <int R, int D, int NQ, int SETS = 1>
 struct DealtLds {
   static constexpr bool kQueries = R > 2 || NQ > 1;
   static constexpr int kState = R * (D / 16) * 256 + 2 * R * 16;                    // floats: O as [row tile][channel tile][lane] vectors, references, sums
   static constexpr int kQueryFloats = kQueries ? NQ * R * (D / 32) * 256 : 0;
   static constexpr int kTile = 32 * D + 64 * (D / 32);                              // bytes of a tile: keys, values, scales
+  // two workgroups to a compute unit, with the plan of some 64 heads each
+  static constexpr int kRoom = 80 * 1024 - 64 * 32 - kQueryFloats * 4;
+  static constexpr int kRing = kRoom >= kWaves * 4 * kTile ? 4 : 3;                 // tiles
   // LDS images of the wavefronts' states: all of them, or where there is no room for that half (each wavefront of the second half hands its state
   // to one of the first, before those hand theirs to everybody)
-  static constexpr bool kAll = (kQueryFloats + kWaves * kState) * 4 + kPlannedHeads * 32 <= 160 * 1024;
+  static constexpr bool kAll = kRoom >= kWaves * kState * 4;
   static constexpr int kSlots = (kAll ? kWaves : kWaves / 2) / SETS;                // of a set
   static constexpr int kRingBytes = kWaves * kRing * kTile, kStateBytes = SETS * kSlots * kState * 4;   // (one after the other in the same place)
   static constexpr int kBytes = kQueryFloats * 4 + (kRingBytes > kStateBytes ? kRingBytes : kStateBytes);
@@ -325,7 +329,7 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
   constexpr int kPageBytes = GP * D / 2, kPageScales = 2 * GP * J;
   typedef DealtLds<R, D, NQ, SETS> Lds;
   static_assert(SETS == 1 || (!Lds::kQueries && Lds::kAll), "the sets' queries are not the same, and a wavefront hands its state to one of its set");
-  constexpr bool kTight = D == 128 && Lds::kQueries;   // registers are short
+  constexpr int kRing = Lds::kRing;
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));   // (what derives from it is worked out per segment, not kept in registers over all of them)
   const int in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_group % WAVES, set = in_group / WAVES;
@@ -407,12 +411,12 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
     if (lane < kPieces * PPT)
       start_to_lds(pk.scales + (lane < kPieces ? t0 : t1) * kPageScales + lane % kPieces * 16, to + 32 * D);
   };
-#pragma unroll
-  for (int n = 0; n < kRing - 1; ++n) {
+  auto start_first = [&](int n) {
     start_tile(n, n);
     nv[n][0] = nv[kRing - 1][0];
     nv[n][1] = nv[kRing - 1][1];
-  }
+  };
+  start_first(0);
 
   // ---- query rows, in the order the keys' channels are contracted in: fragment (row tile, product), its terms
   bf16x8_t qf[Lds::kQueries ? 1 : R][NQ][KS];
@@ -447,6 +451,8 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
       }
     }
   }
+#pragma unroll
+  for (int n = 1; n < kRing - 1; ++n) start_first(n);
   if constexpr (Lds::kQueries) __syncthreads();
 
   float m_run[R], up_thr[R];
@@ -461,45 +467,52 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
     for (int nt = 0; nt < NT; ++nt) o[mt][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   }
 
-  int slot_now = 0, slot_next = kRing - 1;
-  for (int n = 0; n < ntw; ++n) {
-    if ((n + kRing - 1) % TPR == 0) {   // (the entries are decoded behind the branch, so nothing waits where it joins)
-      const int next = listed(n + kRing - 1);
-      decode(next, entry(next));
-    }
-    start_tile(n + kRing - 1, slot_next);
-    landed<kLoads * (kRing - 1)>();
-    const char* tile = ring + slot_now * Lds::kTile;
+  // Scores of the tile in ring slot `slot`.
+  auto score = [&](int slot, f32x4_t (&sc)[R][2]) {
+    const char* tile = ring + slot * Lds::kTile;
     const uint8_t* scales = reinterpret_cast<const uint8_t*>(tile + 32 * D);
-    // scores, a subtile at a time (the barriers keep what is read or converted ahead, and so the registers, to that)
-    f32x4_t sc[R][2];
+    bf16x8_t kf[2][KS];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       uint32_t c[W];
       lds_dwords<W>(tile + (D == 128 ? s * 1024 + lane * 16 : s * 512 + l16 * 32 + qd * 8), c);
       const float scale = power_of(scales[(GP == 16 ? s * kPageScales + l16 * J : (16 * s + l16) * J) + qd * CPL / 32]);
-      bf16x8_t kf[KS];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        kf[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(codes_to_bf16<0>(c[ks], scale), codes_to_bf16<1>(c[ks], scale),
-                                                         codes_to_bf16<2>(c[ks], scale), codes_to_bf16<3>(c[ks], scale)));
-#pragma unroll
-      for (int mt = 0; mt < R; ++mt) {
-        sc[mt][s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-          for (int t = NQ - 1; t >= 0; --t) {
-            bf16x8_t q;
-            if constexpr (Lds::kQueries)
-              q = q_lds[((mt * KS + ks) * NQ + t) * 64 + lane];
-            else
-              q = qf[mt][t][ks];
-            sc[mt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks], q, sc[mt][s], 0, 0, 0);
-          }
-      }
-      if constexpr (kTight) __builtin_amdgcn_sched_barrier(0);
+        kf[s][ks] = __builtin_bit_cast(bf16x8_t, make_uint4(codes_to_bf16<0>(c[ks], scale), codes_to_bf16<1>(c[ks], scale),
+                                                            codes_to_bf16<2>(c[ks], scale), codes_to_bf16<3>(c[ks], scale)));
     }
+#pragma unroll
+    for (int mt = 0; mt < R; ++mt) {
+      sc[mt][0] = sc[mt][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int t = NQ - 1; t >= 0; --t) {
+          bf16x8_t q;
+          if constexpr (Lds::kQueries)
+            q = q_lds[((mt * KS + ks) * NQ + t) * 64 + lane];
+          else
+            q = qf[mt][t][ks];
+          sc[mt][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0][ks], q, sc[mt][0], 0, 0, 0);
+          sc[mt][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1][ks], q, sc[mt][1], 0, 0, 0);
+        }
+    }
+  };
+  // A tile's scores are made beside the numerators and value products of the one before it: the matrix core works on the ones while the vector units
+  // work on the others.
+  f32x4_t sc[R][2];
+  landed<kLoads * (kRing - 2)>();
+  score(0, sc);
+  int slot_now = 0, slot_start = kRing - 1;
+  for (int n = 0; n < ntw; ++n) {
+    if ((n + kRing - 1) % TPR == 0) {   // (the entries are decoded behind the branch, so nothing waits where it joins)
+      const int next = listed(n + kRing - 1);
+      decode(next, entry(next));
+    }
+    start_tile(n + kRing - 1, slot_start);
+    const char* tile = ring + slot_now * Lds::kTile;
+    const uint8_t* scales = reinterpret_cast<const uint8_t*>(tile + 32 * D);
     uint32_t vc[2][W], vs[2][4];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -523,7 +536,7 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
 #pragma unroll
     for (int mt = 0; mt < R; ++mt) {
       const f32x4_t a = sc[mt][0], c = sc[mt][1];
-      tm[mt] = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3])));
+      tm[mt] = fmaxf(fmaxf(fmaxf(fmaxf(a[0], a[1]), a[2]), fmaxf(fmaxf(a[3], c[0]), c[1])), fmaxf(c[2], c[3]));
       any_up |= tm[mt] > up_thr[mt];
     }
     if (__any(any_up)) {
@@ -541,6 +554,11 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
         }
       }
     }
+    landed<kLoads * (kRing - 2)>();   // the next tile
+    slot_start = slot_now;
+    slot_now = slot_now == kRing - 1 ? 0 : slot_now + 1;
+    f32x4_t next_sc[R][2];
+    score(slot_now, next_sc);         // (behind the last tile: of the pool's first page, for nothing)
     f16x8_t p_hi[R], p_lo[R];
 #pragma unroll
     for (int mt = 0; mt < R; ++mt) {
@@ -554,7 +572,6 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
       for (int s = 0; s < 2; ++s) value_operands(vc[s][g], vs[s], g, lo[s], hi[s]);
       const f16x8_t va = __builtin_bit_cast(f16x8_t, make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y));
       const f16x8_t vb = __builtin_bit_cast(f16x8_t, make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y));
-      if constexpr (kTight) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) {
         o[mt][2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, p_hi[mt], o[mt][2 * g], 0, 0, 0);
@@ -566,13 +583,23 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
         o[mt][2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, p_lo[mt], o[mt][2 * g + 1], 0, 0, 0);
       }
     }
+    // one matrix instruction, a few vector ones, in turn (and a query fragment from LDS just ahead of its product, not all of them)
+#pragma unroll
+    for (int i = 0; i < R * (2 * KS * NQ + 2 * NT + 2); ++i) {
+      if (Lds::kQueries && i < R * 2 * KS * NQ && i % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+    }
+#pragma unroll
+    for (int mt = 0; mt < R; ++mt) {
+      sc[mt][0] = next_sc[mt][0];
+      sc[mt][1] = next_sc[mt][1];
+    }
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i) {
       nv[i][0] = nv[i + 1][0];
       nv[i][1] = nv[i + 1][1];
     }
-    slot_now = slot_now == kRing - 1 ? 0 : slot_now + 1;
-    slot_next = slot_next == kRing - 1 ? 0 : slot_next + 1;
   }
 
   // ---- the wavefronts' states become one partial, in a fixed order, each wavefront making some of its vectors
@@ -894,27 +921,36 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_counted_kernel(LOSA_P
   });
 }
 
-// ---- joins a list's partials: a workgroup per row (of a few, in turn), 1024 / D lanes of items times D / 4 channel quads, eight items of a lane at
-// once; sums in a fixed order.
+// ---- joins a list's partials, in the order of the items.  D / 4 threads have a row's channels, four each.  Up to kFewItems items: those threads take all of them
+// one after the other, eight requested at once, and a workgroup has 1024 / D rows.  More: a workgroup has a row, 1024 / D lanes of items.
+constexpr int kFewItems = 16;
 template <int D>
 __global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, AttnInputs in, Partials part, PackedOut out) {
   constexpr int C4 = D / 4, CL = 256 / C4, KB = 8;
   __shared__ __attribute__((aligned(16))) float4 red[CL][C4];
   __shared__ float2 stats[CL];
-  const int tid = threadIdx.x, cl = tid / C4, c4 = tid % C4, head = blockIdx.y, b = head / sh.Hkv, j = head - b * sh.Hkv;
-  const int2 table = out.table[head];
-  const int M = min(active_rows(in, kv, sh, b), min(sh.rows_max, part.rows));
-  if (table.y == 1) return;   // finished already
-  for (int r = blockIdx.x; r < M; r += gridDim.x) {
-    const int a = row_token(sh, r), tok = in.active_idx ? in.active_idx[(size_t)b * sh.B + a] : a;
-    float m = kNegBig, l = 0.f;
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = cl; i0 < table.y; i0 += CL * KB) {
+  const int tid = threadIdx.x, cl = tid / C4, c4 = tid % C4, head = blockIdx.y, b = head / sh.Hkv;
+  int n = __builtin_amdgcn_readfirstlane((in.active_count ? in.active_count : kv.seq_lens)[b]);
+  int first = __builtin_amdgcn_readfirstlane(out.table[head].x), items = __builtin_amdgcn_readfirstlane(out.table[head].y);
+  asm("" : "+s"(n), "+s"(first), "+s"(items) : "s"(sh.B), "s"(sh.G));   // (one memory round trip; see Sequence)
+  if (items == 1) return;   // finished already
+  const int M = min((in.active_count ? min(n, sh.B) : sh.B) * sh.G, min(sh.rows_max, part.rows));
+  const bool few = items <= kFewItems;
+  Segment s;
+  s.b = b;
+  s.j = head - b * sh.Hkv;
+  s.item = -1;
+  // items lane, lane + step, ... of row r
+  auto gather = [&](int r, int lane, int step, float& m, float& l, f32x4_t& acc) {
+    m = kNegBig;
+    l = 0.f;
+    acc = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    for (int i0 = lane; i0 < items; i0 += step * KB) {
       float mk[KB], lk[KB];
       f32x4_t x[KB];
 #pragma unroll
       for (int k = 0; k < KB; ++k) {
-        const uint32_t prow = (uint32_t)(table.x + min(i0 + CL * k, table.y - 1)) * part.rows + r;
+        const uint32_t prow = (uint32_t)(first + min(i0 + step * k, items - 1)) * part.rows + r;
         mk[k] = part.m[prow];
         lk[k] = part.l[prow];
         x[k] = reinterpret_cast<const f32x4_t*>(part.o + (size_t)prow * D)[c4];
@@ -922,7 +958,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, A
       float m_new = m;
 #pragma unroll
       for (int k = 0; k < KB; ++k) {
-        if (i0 + CL * k >= table.y) mk[k] = kNegBig, lk[k] = 0.f, x[k] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        if (i0 + step * k >= items) mk[k] = kNegBig, lk[k] = 0.f, x[k] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
         m_new = fmaxf(m_new, mk[k]);
       }
       const float keep = __builtin_amdgcn_exp2f(m - m_new);
@@ -936,10 +972,24 @@ __global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, A
         acc += x[k] * wgt;
       }
     }
+  };
+  if (few) {
+    for (int r = blockIdx.x * CL + cl; r < M; r += gridDim.x * CL) {
+      float m, l;
+      f32x4_t acc;
+      gather(r, 0, 1, m, l, acc);
+      store_state<D>(sh, in, part, out, s, r, c4 * 4, acc, m, l);
+    }
+    return;
+  }
+  for (int r = blockIdx.x; r < M; r += gridDim.x) {
+    float m, l;
+    f32x4_t acc;
+    gather(r, cl, CL, m, l, acc);
     red[cl][c4] = make_float4(acc[0], acc[1], acc[2], acc[3]);
     if (c4 == 0) stats[cl] = make_float2(m, l);
     __syncthreads();
-    if (tid < C4 && (unsigned)tok < (unsigned)sh.B) {
+    if (tid < C4) {
       float m_all = kNegBig, l_all = 0.f;
       f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -951,10 +1001,6 @@ __global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, A
         l_all = fmaf(stats[k].y, wgt, l_all);
         o += (f32x4_t){x.x, x.y, x.z, x.w} * wgt;
       }
-      Segment s;
-      s.b = b;
-      s.j = j;
-      s.item = -1;
       store_state<D>(sh, in, part, out, s, r, c4 * 4, o, m_all, l_all);
     }
     __syncthreads();   // the LDS is the next row's
@@ -966,14 +1012,14 @@ typedef void (*PackedKernel)(LOSA_PACKED_ARGS);
 template <int D, int GP>
 static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, int heads, int workgroups,
                             int least_tiles, int rows, bool known, const Partials& part, const PackedOut& out) {
-  auto go = [&](PackedKernel kern, int lds_bytes, bool& attr_set) {
+  auto go = [&](PackedKernel kern, int lds_bytes, bool& attr_set, int waves = kWaves) {
     const int all = lds_bytes + (workgroups ? heads * 32 : 0);   // the plan behind the kernel's own
     if (!attr_set) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes + kPlannedHeads * 32);
       if (e != hipSuccess) return e;
       attr_set = true;
     }
-    kern<<<workgroups ? workgroups : heads, 512, all, st>>>(kv, sh, in, pk, part, out, sh.sm_scale * 1.4426950408889634f, heads, workgroups, least_tiles);
+    kern<<<workgroups ? workgroups : heads, 64 * waves, all, st>>>(kv, sh, in, pk, part, out, sh.sm_scale * 1.4426950408889634f, heads, workgroups, least_tiles);
     return hipGetLastError();
   };
   static bool set[10];   // per kernel
@@ -986,7 +1032,7 @@ static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const S
   if (rows <= 32) return go(packed_attn_kernel<D, GP, 2, 1>, DealtLds<2, D, 1>::kBytes, set[5]);
   if (rows <= 48) return go(packed_attn_kernel<D, GP, 3, 1>, DealtLds<3, D, 1>::kBytes, set[6]);
   if (rows <= 64) return go(packed_attn_kernel<D, GP, 2, 1, 2>, DealtLds<2, D, 1, 2>::kBytes, set[7]);
-  return rows <= 128 ? go(packed_rows_kernel<D, GP, 1>, 2 * kStageBytes<D>, set[8]) : go(packed_rows_kernel<D, GP, 2>, 2 * kStageBytes<D>, set[9]);
+  return rows <= 128 ? go(packed_rows_kernel<D, GP, 1>, 2 * kStageBytes<D>, set[8], 8) : go(packed_rows_kernel<D, GP, 2>, 2 * kStageBytes<D>, set[9], 8);
 }
 
 hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk, int workgroups,
@@ -997,9 +1043,11 @@ hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const
   return launch(st, dtype, kv, sh, in, pk, heads, workgroups, least_tiles, rows, rows_known, part, out);
 }
 
-hipError_t launch_packed_join(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, int rows, bool rows_known, const Partials& part,
-                              const PackedOut& out) {
-  const dim3 grid(rows_known ? rows : min(rows, 64), batch * sh.Hkv);   // (rows that only the device counts are mostly few)
+hipError_t launch_packed_join(hipStream_t st, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, int workgroups, int rows, bool rows_known,
+                              const Partials& part, const PackedOut& out) {
+  const int heads = batch * sh.Hkv, per_group = 1024 / sh.d, likely = rows_known ? rows : min(rows, 64);   // (rows that only the device counts are mostly few)
+  // (how many items a list has is the device's to know; on average no more than these)
+  const dim3 grid(workgroups / heads + 2 <= kFewItems ? (likely + per_group - 1) / per_group : likely, heads);
   if (sh.d == 128)
     packed_join_kernel<128><<<grid, 256, 0, st>>>(kv, sh, in, part, out);
   else
