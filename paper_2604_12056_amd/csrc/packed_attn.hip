@@ -157,7 +157,8 @@ __device__ __forceinline__ f32x4_t sum_of(const f16x8_t& p_hi, const f16x8_t& p_
 // cut into equal shares, one per workgroup: lists of any lengths keep every compute unit busy to the end.  A share that ends inside a list leaves a
 // partial, and the merge kernel joins a list's partials; a list that lies in one share is finished by its workgroup.
 // Every workgroup works the cut out for itself from the counts (one memory round trip and a prefix sum): lists in the order of their
-// heads, list h at [start, start + tiles * unit).  Tile t is workgroup (start + t * unit) / share's.  The partial of workgroup w for list h is item w + h.
+// heads, list h at [start, start + tiles * unit), and ahead of each the time that its start and its end take, as tiles (GAP: some 10 us where four
+// wavefronts deal tiles out; without it a workgroup with the end of one list and the start of another took twice the others' time).  Tile t is workgroup (start + t * unit) / share's.  The partial of workgroup w for list h is item w + h.
 // Beyond kPlannedHeads lists every one has a workgroup of its own.
 struct Segment {
   int b, j, head, M;               // M: query rows
@@ -178,7 +179,7 @@ __device__ __forceinline__ int quotient(int a, int b) {
 }
 
 // BLOCK: query rows that convert a tile once.  f(segment) for every list of this workgroup, in order.
-template <int GP, int BLOCK, typename F>
+template <int GP, int BLOCK, int GAP, typename F>
 __device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& sh, const AttnInputs& in, const Partials& part, const PackedOut& out, int heads,
                                                  int workgroups, int least_tiles, int* plan, F f) {
   constexpr int PPT = 32 / GP;
@@ -209,10 +210,10 @@ __device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& 
     const Sequence seq = sequence_of(kv, sh, b);
     n = (in.active_count ? min(n, sh.B) : sh.B) * sh.G;
     const int M = h0 + lane < heads ? min(n, min(sh.rows_max, part.rows)) : 0, pages = in.list ? max(0, min(min(listed, in.cap), sh.max_pages)) : seq.pages;
-    const int unit = unit_cost(M, BLOCK), tiles = M > 0 ? (pages + PPT - 1) / PPT : 0, cost = tiles * unit;
+    const int unit = unit_cost(M, BLOCK), tiles = M > 0 ? (pages + PPT - 1) / PPT : 0, cost = tiles > 0 ? (GAP + tiles) * unit : 0;
     const int incl = wave_inclusive_scan(cost);
     if (h0 + lane < heads) {
-      heads_plan[2 * h] = make_int4(total + incl - cost, tiles, unit, pages);
+      heads_plan[2 * h] = make_int4(total + incl - tiles * unit, tiles, unit, pages);
       heads_plan[2 * h + 1] = make_int4(M, seq.base, seq.tokens, seq.pages);
     }
     total += __builtin_amdgcn_readlane(incl, 63);
@@ -302,7 +303,7 @@ __device__ __forceinline__ void landed() {
 //   the query fragments are read from LDS for every tile where there are more than two row tiles (or float queries).
 // Four row tiles do not fit.  They are two sets of two (SETS): a wavefront of each set takes every tile, which reads its codes from
 // the cache the second time and converts them twice, 128 of some 240 vector instructions a tile.
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kDealtGap = 16;
 template <int R, int D, int NQ, int SETS = 1>
 struct DealtLds {
   static constexpr bool kQueries = R > 2 || NQ > 1;
@@ -881,7 +882,7 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(LOSA_PACKED_AR
   extern __shared__ __attribute__((aligned(16))) float lds[];
   constexpr int kRows = SETS * R * 16;
   int* plan = reinterpret_cast<int*>(lds) + DealtLds<R, D, NQ, SETS>::kBytes / 4;
-  for_each_segment<GP, kRows>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
+  for_each_segment<GP, kRows, kDealtGap>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
     for (int row0 = 0; row0 < s.M; row0 += kRows) packed_attn_body<D, GP, R, NQ, SETS>(kv, sh, in, pk, s, row0, part, out, scale_log2e, lds);
   });
 }
@@ -891,7 +892,7 @@ __global__ __launch_bounds__(512) void packed_rows_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   constexpr int kRows = 128 * R;
   int* plan = reinterpret_cast<int*>(lds) + 2 * kStageBytes<D> / 4;
-  for_each_segment<GP, kRows>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
+  for_each_segment<GP, kRows, 4>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
     for (int row0 = 0; row0 < s.M; row0 += kRows) packed_rows_body<D, GP, R>(kv, sh, in, pk, s, row0, part, out, scale_log2e, reinterpret_cast<char*>(lds));
   });
 }
@@ -904,7 +905,7 @@ template <int D, int GP, int NQ>
 __global__ __launch_bounds__(64 * kWaves) void packed_attn_counted_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   int* plan = reinterpret_cast<int*>(lds) + kCountedBytes<D, NQ> / 4;
-  for_each_segment<GP, kCountedRows<NQ>>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
+  for_each_segment<GP, kCountedRows<NQ>, kDealtGap>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
     for (int row0 = 0; row0 < s.M; row0 += kCountedRows<NQ>) {
       const int left = s.M - row0;
       if (left <= 16)
