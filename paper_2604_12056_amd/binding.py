@@ -199,6 +199,9 @@ class Context:
 
     def __init__(self, handle: int, workspace, cfg: losa_config):
         self.handle, self.workspace, self.cfg = handle, workspace, cfg
+        # what every call with rows of heads asks for (a structure's field takes as long as a launch's tenth)
+        self.q_heads, self.kv_heads, self.head_dim = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+        self.element_size = 2 if cfg.dtype == LOSA_BF16 else 4
 
     def close(self):
         if self.handle:
@@ -302,73 +305,72 @@ def losa_step(ctx: Context, kv: PagedKV, step_index: int, h_cur, h_prev, q, mode
                                         _ptr(mask), _ptr(sel_count)))
 
 
-def _row_stride(t, ctx: Context, heads: int, what: str) -> int:
+def _row_stride(t, ctx: Context, tokens: int, heads: int, what: str) -> int:
     """Elements between consecutive tokens of a [tokens, heads, d] tensor of the context's type, whose heads have to lie together."""
-    cfg = ctx.cfg
-    d = cfg.head_dim
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.element_size() != (2 if cfg.dtype == LOSA_BF16 else 4):
-        raise LosaError(LOSA_ERR_INVALID_ARG, f"{what} is not a [tokens, {heads}, {d}] tensor of the context's type")
-    if t.shape[0] == 0:
+    d = ctx.head_dim
+    if t.shape != (tokens, heads, d) or t.element_size() != ctx.element_size:
+        raise LosaError(LOSA_ERR_INVALID_ARG, f"{what} is not a [{tokens}, {heads}, {d}] tensor of the context's type")
+    if tokens == 0:
         return 0
     row, head, channel = t.stride()
     if channel != 1 or (head != d and heads > 1):
         raise LosaError(LOSA_ERR_INVALID_ARG, f"{what}: the heads of a token do not lie one behind the other")
-    if t.shape[0] == 1:
+    if tokens == 1:
         return 0
     if row == 0:
         raise LosaError(LOSA_ERR_INVALID_ARG, f"{what}: all tokens are the same row")
     return row
 
 
-def _same(what: str, *sizes: int) -> int:
-    if len(set(sizes)) > 1:
-        raise LosaError(LOSA_ERR_INVALID_ARG, f"{what}: {sizes} tokens do not agree")
-    return sizes[0]
-
-
 def losa_rotate(ctx: Context, rotation: Rotation, positions, q=None, q_out=None, k=None, k_out=None, stream=None):
     """q [tokens, Hq, d] and / or k [tokens, Hkv, d], turned by the positions (int32 [tokens]) into q_out / k_out (the inputs
     themselves, if need be)."""
-    Hq, Hkv = ctx.cfg.num_q_heads, ctx.cfg.num_kv_heads
-    strides = [0 if t is None else _row_stride(t, ctx, h, w) for t, h, w in
-               ((q, Hq, "q"), (q_out, Hq, "q_out"), (k, Hkv, "k"), (k_out, Hkv, "k_out"))]
-    tokens = _same("losa_rotate", int(positions.numel()), *(int(t.shape[0]) for t in (q, q_out, k, k_out) if t is not None))
-    r = rotation.as_struct()
-    _check(ctx, load_library().losa_rotate(ctx.handle, _stream(stream), C.byref(r), _ptr(positions), tokens, _ptr(q), strides[0],
-                                          _ptr(q_out), strides[1], _ptr(k), strides[2], _ptr(k_out), strides[3]))
+    n, qs, qo, ks, ko = positions.numel(), 0, 0, 0, 0
+    if q is not None:
+        qs = _row_stride(q, ctx, n, ctx.q_heads, "q")
+    if q_out is not None:
+        qo = _row_stride(q_out, ctx, n, ctx.q_heads, "q_out")
+    if k is not None:
+        ks = _row_stride(k, ctx, n, ctx.kv_heads, "k")
+    if k_out is not None:
+        ko = _row_stride(k_out, ctx, n, ctx.kv_heads, "k_out")
+    _check(ctx, load_library().losa_rotate(ctx.handle, _stream(stream), C.byref(rotation.as_struct()), positions.data_ptr(), n, _ptr(q), qs,
+                                          _ptr(q_out), qo, _ptr(k), ks, _ptr(k_out), ko))
 
 
 def _new_tokens(ctx: Context, k, v, tok_indptr, positions, max_new_tokens: int) -> losa_new_tokens:
-    h = ctx.cfg.num_kv_heads
-    n = _same("new tokens", int(k.shape[0]), int(v.shape[0]), *(() if positions is None else (int(positions.numel()),)))
-    return losa_new_tokens(_ptr(k), _ptr(v), _row_stride(k, ctx, h, "k"), _row_stride(v, ctx, h, "v"), _ptr(tok_indptr), _ptr(positions),
-                           n, max_new_tokens)
+    n = k.shape[0]
+    if positions is not None and positions.numel() != n:
+        raise LosaError(LOSA_ERR_INVALID_ARG, f"{positions.numel()} positions for {n} tokens")
+    return losa_new_tokens(k.data_ptr(), v.data_ptr(), _row_stride(k, ctx, n, ctx.kv_heads, "k"), _row_stride(v, ctx, n, ctx.kv_heads, "v"),
+                           tok_indptr.data_ptr(), _ptr(positions), n, max_new_tokens)
 
 
 def losa_append_kv(ctx: Context, kv: PagedKV, k, v, tok_indptr, rotation: Optional[Rotation] = None, positions=None,
                    max_new_tokens: int = 0, stream=None):
     """Tokens k, v [tokens, Hkv, d] (row strides as they are) into the pages and bounds of `kv`, whose seq_lens count them already."""
-    s, n, r = kv.as_struct(), _new_tokens(ctx, k, v, tok_indptr, positions, max_new_tokens), rotation and rotation.as_struct()
-    _check(ctx, load_library().losa_append_kv(ctx.handle, _stream(stream), C.byref(s), C.byref(n), C.byref(r) if r else None))
+    _check(ctx, load_library().losa_append_kv(ctx.handle, _stream(stream), C.byref(kv.as_struct()),
+                                             C.byref(_new_tokens(ctx, k, v, tok_indptr, positions, max_new_tokens)),
+                                             None if rotation is None else C.byref(rotation.as_struct())))
 
 
 def losa_append_packed(ctx: Context, kv: PackedKV, k, v, tok_indptr, rotation: Optional[Rotation] = None, positions=None,
                        max_new_tokens: int = 0, stream=None):
     """The same into a 4-bit cache."""
-    s, n, r = kv.as_struct(), _new_tokens(ctx, k, v, tok_indptr, positions, max_new_tokens), rotation and rotation.as_struct()
-    _check(ctx, load_library().losa_append_packed(ctx.handle, _stream(stream), C.byref(s), C.byref(n), C.byref(r) if r else None))
+    _check(ctx, load_library().losa_append_packed(ctx.handle, _stream(stream), C.byref(kv.as_struct()),
+                                                 C.byref(_new_tokens(ctx, k, v, tok_indptr, positions, max_new_tokens)),
+                                                 None if rotation is None else C.byref(rotation.as_struct())))
 
 
 def losa_read_packed(ctx: Context, kv: PackedKV, tok_indptr, k_out, v_out, max_tokens: int = 0, stream=None):
     """The last tokens of every sequence of a 4-bit cache into k_out / v_out [tokens, Hkv, d] (contiguous; either may be None)."""
-    outs = [t for t in (k_out, v_out) if t is not None]
-    for t in outs:
-        if _row_stride(t, ctx, ctx.cfg.num_kv_heads, "an output") and not t.is_contiguous():
+    one = k_out if k_out is not None else v_out
+    n = 0 if one is None else one.shape[0]
+    for t in (k_out, v_out):
+        if t is not None and _row_stride(t, ctx, n, ctx.kv_heads, "an output") not in (0, ctx.kv_heads * ctx.head_dim):
             raise LosaError(LOSA_ERR_INVALID_ARG, "outputs are contiguous")
-    tokens = _same("outputs", *(int(t.shape[0]) for t in outs)) if outs else 0
-    s = kv.as_struct()
-    _check(ctx, load_library().losa_read_packed(ctx.handle, _stream(stream), C.byref(s), _ptr(tok_indptr), tokens, max_tokens, _ptr(k_out),
-                                               _ptr(v_out)))
+    _check(ctx, load_library().losa_read_packed(ctx.handle, _stream(stream), C.byref(kv.as_struct()), _ptr(tok_indptr), n, max_tokens,
+                                               _ptr(k_out), _ptr(v_out)))
 
 
 def losa_sparse_attn_packed(ctx: Context, kv: PackedKV, q, active_idx, active_count, sel_pages, sel_count, cap: int, o_p, lse_p,

@@ -116,14 +116,15 @@ def test_binding_refuses_rows_it_cannot_describe():
                         max_pages_per_seq=4, max_topk_pages=1)
     ctx = L.Context(None, None, cfg)
     x = torch.zeros((6, 8, 64), dtype=torch.bfloat16)
-    assert L._row_stride(x[:, 2:4], ctx, 2, "k") == 512 and L._row_stride(x[:1, 2:4], ctx, 2, "k") == 0
-    assert L._row_stride(x[::2, 2:4], ctx, 2, "k") == 1024
-    for bad in (x, x[:, ::4], x[:, 2:4].float(), x[:, 2:4].transpose(0, 1), x[:1, :2].expand(6, 2, 64), x[..., :32][:, :2]):
+    assert L._row_stride(x[:, 2:4], ctx, 6, 2, "k") == 512 and L._row_stride(x[:1, 2:4], ctx, 1, 2, "k") == 0
+    assert L._row_stride(x[::2, 2:4], ctx, 3, 2, "k") == 1024
+    for bad in (x, x[:, ::4], x[:, 2:4].float(), x[:, 2:4].transpose(0, 1), x[:1, :2].expand(6, 2, 64), x[..., :32][:, :2], x[:5, :2], x[0]):
         with pytest.raises(L.LosaError) as e:
-            L._row_stride(bad, ctx, 2, "k")
+            L._row_stride(bad, ctx, 6, 2, "k")
         assert e.value.status == INV
     rot = L.Rotation(torch.zeros((8, 64)))
     with pytest.raises(L.LosaError):
         L.losa_rotate(ctx, rot, torch.zeros(5, dtype=torch.int32), x[:, :4], x[:, :4].clone())   # five positions, six tokens
-    with pytest.raises(L.LosaError):
-        L._new_tokens(ctx, x[:, :2], x[:5, :2], None, None, 0)
+    for k, v, positions in ((x[:, :2], x[:5, :2], None), (x[:, :2], x[:, :2], torch.zeros(5, dtype=torch.int32))):
+        with pytest.raises(L.LosaError):
+            L._new_tokens(ctx, k, v, torch.zeros(2, dtype=torch.int32), positions, 0)
