@@ -88,9 +88,11 @@ __global__ __launch_bounds__(256) void append_kernel(KvView kv, Shape sh, NewTok
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Fill f = fill_of(kv, sh, in.indptr, in.num_tokens, blockIdx.y, blockIdx.x);
   if (f.hi <= f.lo) return;
+  const int phys = kv.page_indices[f.entry];
+  if ((unsigned)phys >= (unsigned)kv.num_pages) return;
   const Unit u = unit_of<V>(lane % LPT, rot.table ? rot.rotary : 0, rot.pairs);
   for (int j = wave; j < sh.Hkv; j += 4) {
-    const size_t tile = (size_t)f.phys * sh.Hkv + j;
+    const size_t tile = (size_t)phys * sh.Hkv + j;
     uint32_t there = 0;   // rows that hold a token now
     T* rows = lds[wave];
 #pragma unroll

@@ -82,26 +82,21 @@ __device__ __forceinline__ uint4 round16(const float (&f)[4], float) {
 }
 
 // ---- the page a workgroup fills
-// Rows lo .. hi-1 of page `phys` take the new tokens from row `source` of k and v on; the first of them is token `slot` of the sequence.
+// Rows lo .. hi-1 of a page take the new tokens from row `source` of k and v on; the first of them is token `slot` of the sequence.
 struct Fill {
-  int phys, lo, hi, source, slot;
+  int entry, lo, hi, source, slot;   // entry: the page's place in page_indices
 };
 // The `tile`-th page of sequence b that gets new tokens; hi <= lo where there is none.
-// The sequence's last n tokens are the new ones; tokens whose page is not listed, not in the pool or beyond the
-// launch's bound are left out.
+// The sequence's last n tokens are the new ones; tokens whose page is not listed or beyond the launch's bound are left out.
+// (Whether the page is in the pool is the caller's to check, with other loads already on their way.)
 __device__ __forceinline__ Fill fill_of(const KvView& kv, const Shape& sh, const int32_t* indptr, int num_tokens, int b, int tile) {
   const int t0 = max(indptr[b], 0), t1 = min(indptr[b + 1], num_tokens), len = max(kv.seq_lens[b], 0);
   const int base = kv.page_indptr[b], listed = kv.page_indptr[b + 1] - base;
   const int n = t1 - t0, first = len - n, begin = max(first, 0), shift = sh.g == 16 ? 4 : 5;
   const int p = (begin >> shift) + tile;
-  Fill f = {-1, 0, 0, 0, 0};
-  if (n <= 0 || p >= min(min(listed, sh.max_pages), kv.seq_page_limit)) return f;
-  const int lo = max(begin - (p << shift), 0), hi = min(len - (p << shift), sh.g);
-  if (hi <= lo) return f;
-  const int phys = kv.page_indices[base + p];
-  if ((unsigned)phys >= (unsigned)kv.num_pages) return f;
-  const int slot = (p << shift) + lo;
-  return {phys, lo, hi, t0 + (slot - first), slot};
+  if (n <= 0 || p >= min(min(listed, sh.max_pages), kv.seq_page_limit)) return {0, 0, 0, 0, 0};
+  const int lo = max(begin - (p << shift), 0), hi = min(len - (p << shift), sh.g), slot = (p << shift) + lo;
+  return {base + p, lo, hi, t0 + (slot - first), slot};
 }
 // Pages that n tokens can touch at most.
 inline int pages_touched(int n, int g) { return n <= 0 ? 0 : (int)(((long)n + 2 * g - 2) / g); }

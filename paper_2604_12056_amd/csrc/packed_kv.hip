@@ -1,8 +1,9 @@
 // New tokens into a 4-bit cache, and tokens out of it.
 //
-// A lane has one token's group of 32 channels: what a scale is made of, and the 16 bytes that come of it.  With 128 channels the
-// 64 lanes are the sixteen tokens of a page or of half of one, and 16 bytes a lane are what a page-head tile holds in lane order.
-// A workgroup has one page, each of its four wavefronts every fourth KV head of it.
+// Bytes are all there is to them, so what matters is that a wavefront asks for all of its own before it uses any, and stores whole lines.
+// Packing: a lane has one token's group of 32 channels, what a scale is made of, and the 16 bytes that come of it; a wavefront has
+// 16 tokens of a page and head (32 with 64 channels in a page of 32).  Reading: a lane has eight channels of a token, 16 bytes of what is
+// written.  A workgroup is four wavefronts of a page: two halves of two heads, or four heads.
 #include "losa_device.h"
 #include "losa_internal.h"
 #include "new_tokens.h"
@@ -10,65 +11,95 @@
 
 namespace losa {
 
-// 32 channels of a row, widened.
+// 32 channels of a row as they lie, and widened.
 template <typename T>
-__device__ __forceinline__ void load32(const T* p, float (&x)[32]) {
+struct Raw32 {
+  uint4 v[32 / Vec16<T>::n];
+};
+template <typename T>
+__device__ __forceinline__ Raw32<T> load32(const T* p) {
+  Raw32<T> r;
+#pragma unroll
+  for (int i = 0; i < 32 / Vec16<T>::n; ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen32(const Raw32<T>& r, float (&x)[32]) {
   constexpr int V = Vec16<T>::n;
 #pragma unroll
-  for (int e = 0; e < 32; e += V) {
+  for (int i = 0; i < 32 / V; ++i) {
     float f[V];
-    widen16(*reinterpret_cast<const uint4*>(p + e), f, T());
+    widen16(r.v[i], f, T());
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[e + i] = f[i];
+    for (int e = 0; e < V; ++e) x[V * i + e] = f[e];
   }
 }
 
-// Channels c .. c + 31 of `row`, turned by the angles of one position (`angles`: cosines, then sines) and rounded to T, as a cache of T would
-// hold them.  Eight channels are turned by a whole half or not at all, as rotary_dim is a multiple of 16.
+// What turns channels c .. c + 31 of a row: their angles and, halves style, the channels half a turn's width away.  Eight channels are turned by a whole
+// half or not at all, as rotary_dim is a multiple of 16.  (No branch around a load: what does not turn, or has its pair at hand, loads something and
+// does not use it.)
 template <typename T>
-__device__ __forceinline__ void load32_turned(const T* row, int c, const float* angles, const Rotation& rot, float (&x)[32]) {
-  load32<T>(row + c, x);
+struct Turn32 {
+  float4 cs[8], sn[8];   // pairs style: every other one counts
+  uint4 other[32 / Vec16<T>::n];
+};
+template <typename T>
+__device__ __forceinline__ void load_turn32(const T* row, int c, const float* angles, const Rotation& rot, Turn32<T>& t) {
+  constexpr int V = Vec16<T>::n;
+  const int half = rot.rotary / 2, next = rot.pairs ? 0 : 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int ch = c + 8 * i, in = ch < rot.rotary ? ch : 0;
+    const int at = rot.pairs ? in / 2 : in < half ? in : in - half;
+    const int away = rot.pairs || ch >= rot.rotary ? ch : ch < half ? ch + half : ch - half;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      t.cs[2 * i + k] = *reinterpret_cast<const float4*>(angles + at + next * k);
+      t.sn[2 * i + k] = *reinterpret_cast<const float4*>(angles + half + at + next * k);
+    }
+#pragma unroll
+    for (int k = 0; k < 8 / V; ++k) t.other[8 / V * i + k] = *reinterpret_cast<const uint4*>(row + away + V * k);
+  }
+}
+// x, turned and rounded to T, as a cache of T would hold it.
+template <typename T>
+__device__ __forceinline__ void turn32(float (&x)[32], int c, const Rotation& rot, const Turn32<T>& t) {
+  constexpr int V = Vec16<T>::n;
   const int half = rot.rotary / 2;
 #pragma unroll
-  for (int e = 0; e < 32; e += 8) {
-    const int ch = c + e;
-    if (ch >= rot.rotary) continue;
+  for (int i = 0; i < 4; ++i) {
+    const int ch = c + 8 * i;
     float y[8];
     if (rot.pairs) {
-      float cs[4], sn[4];
-      load_floats<4>(angles + ch / 2, cs);
-      load_floats<4>(angles + half + ch / 2, sn);
+      const float4 c0 = t.cs[2 * i], s0 = t.sn[2 * i];
+      const float cs[4] = {c0.x, c0.y, c0.z, c0.w}, sn[4] = {s0.x, s0.y, s0.z, s0.w};
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        y[i] = turned(x[e + i], cs[i / 2], x[e + i + 1], -sn[i / 2]);
-        y[i + 1] = turned(x[e + i + 1], cs[i / 2], x[e + i], sn[i / 2]);
+      for (int e = 0; e < 8; e += 2) {
+        y[e] = turned(x[8 * i + e], cs[e / 2], x[8 * i + e + 1], -sn[e / 2]);
+        y[e + 1] = turned(x[8 * i + e + 1], cs[e / 2], x[8 * i + e], sn[e / 2]);
       }
     } else {
-      const bool second = ch >= half;
-      const int at = second ? ch - half : ch;
-      float cs[8], sn[8], other[8];
-      load_floats<8>(angles + at, cs);
-      load_floats<8>(angles + half + at, sn);
-      constexpr int V = Vec16<T>::n;
+      const float4 c0 = t.cs[2 * i], c1 = t.cs[2 * i + 1], s0 = t.sn[2 * i], s1 = t.sn[2 * i + 1];
+      const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+      float other[8];
 #pragma unroll
-      for (int i = 0; i < 8; i += V) {
+      for (int k = 0; k < 8 / V; ++k) {
         float f[V];
-        widen16(*reinterpret_cast<const uint4*>(row + (second ? at : at + half) + i), f, T());
+        widen16(t.other[8 / V * i + k], f, T());
 #pragma unroll
-        for (int k = 0; k < V; ++k) other[i + k] = f[k];
+        for (int e = 0; e < V; ++e) other[V * k + e] = f[e];
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = turned(x[e + i], cs[i], other[i], second ? sn[i] : -sn[i]);
+      for (int e = 0; e < 8; ++e) y[e] = turned(x[8 * i + e], cs[e], other[e], ch >= half ? sn[e] : -sn[e]);
     }
-    constexpr int V = Vec16<T>::n;
 #pragma unroll
-    for (int i = 0; i < 8; i += V) {
+    for (int k = 0; k < 8; k += V) {
       float f[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) f[k] = y[i + k];
+      for (int e = 0; e < V; ++e) f[e] = y[k + e];
       widen16(round16(f, T()), f, T());
 #pragma unroll
-      for (int k = 0; k < V; ++k) x[e + i + k] = f[k];
+      for (int e = 0; e < V; ++e) x[8 * i + k + e] = ch < rot.rotary ? f[e] : x[8 * i + k + e];
     }
   }
 }
@@ -90,132 +121,156 @@ __device__ __forceinline__ uint4 codes_of(const float (&x)[32], int byte) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+template <int D, int GP>
+struct PageWork {   // of a workgroup
+  static constexpr int J = D / 32, TPP = 64 / J < GP ? 64 / J : GP;   // groups per token, tokens per wavefront
+  static constexpr int PASSES = GP / TPP, HEADS = 4 / PASSES;         // wavefronts per page and head, heads per workgroup
+};
+
 template <typename T, int D, int GP>
 __global__ __launch_bounds__(256) void append_packed_kernel(KvView kv, Shape sh, NewTokens in, Rotation rot, PackedView out) {
-  constexpr int J = D / 32, TPP = 64 / J < GP ? 64 / J : GP;   // groups per token, tokens per pass
-  __shared__ __attribute__((aligned(16))) T lds[4][GP * D];
+  typedef PageWork<D, GP> Work;
+  constexpr int J = Work::J, TPP = Work::TPP, kTile = GP * D / 2;
+  __shared__ __attribute__((aligned(16))) T keys[Work::HEADS][GP * D];   // the numbers that stand for the keys, for the page's bounds
+  __shared__ __attribute__((aligned(16))) uint8_t codes[4][TPP * D / 2];
+  __shared__ uint32_t arrived[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pass = wave % Work::PASSES, hl = wave / Work::PASSES, h = blockIdx.z * Work::HEADS + hl, j = lane % J;
   const Fill f = fill_of(kv, sh, in.indptr, in.num_tokens, blockIdx.y, blockIdx.x);
   if (f.hi <= f.lo) return;
-  const int j = lane % J;
-  for (int h = wave; h < sh.Hkv; h += 4) {
-    const size_t tile = (size_t)f.phys * sh.Hkv + h;
-    uint8_t* scales = out.scales + tile * (2 * GP * J);
-    uint8_t* vcodes = out.v + tile * (GP * D / 2);
-    uint32_t there = 0;
+  const int phys = kv.page_indices[f.entry];
+  const int row = lane / J, t = pass * TPP + row;   // (with 64 channels and pages of 16 the upper lanes have no row)
+  const bool mine = row < TPP && t >= f.lo && t < f.hi && h < sh.Hkv;
+  const int at_row = max(f.lo, min(t, f.hi - 1)) - f.lo, src = f.source + at_row, head = min(h, sh.Hkv - 1);
+  const T* const krow = (const T*)in.k + (size_t)src * in.k_stride + head * D;
+  const Raw32<T> kraw = load32<T>(krow + j * 32), vraw = load32<T>((const T*)in.v + (size_t)src * in.v_stride + head * D + j * 32);
+  bool ok = mine;
+  Turn32<T> turn;
+  if (rot.table) {
+    const int at = in.positions ? in.positions[src] : f.slot + at_row;
+    ok = mine && (unsigned)at < (unsigned)rot.max_positions;
+    load_turn32<T>(krow, j * 32, rot.table + (size_t)(ok ? at : 0) * rot.rotary, rot, turn);
+  }
+  if ((unsigned)phys >= (unsigned)kv.num_pages) return;
+  const size_t tile = (size_t)phys * sh.Hkv + head;
+  uint8_t* const scales = out.scales + tile * (2 * GP * J);
+  uint8_t* const vcodes = out.v + tile * kTile;
+
+  float x[32];
+  widen32<T>(kraw, x);
+  if (rot.table) turn32<T>(x, j * 32, rot, turn);
+  const int byte = scale_byte(largest(x), kKeyScaleMin, kKeyScaleMax);
+  const uint4 c = codes_of<2, 1>(x, byte);
+  if (ok) {
+    *reinterpret_cast<uint4*>(out.k + tile * kTile + t * (D / 2) + j * 16) = c;
+    scales[t * J + j] = (uint8_t)byte;
+    if (kv.meta) {
+      const float scale = power_of(byte);
+      const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-    for (int pass = 0; pass < GP / TPP; ++pass) {
-      const int t = pass * TPP + lane / J;
-      const bool mine = t >= f.lo && t < f.hi;   // (lanes past the page's rows have none)
-      const int src = f.source + (t - f.lo);
-      int at = 0;
-      if (mine && rot.table) at = in.positions ? in.positions[src] : f.slot + (t - f.lo);
-      const bool ok = mine && (!rot.table || (unsigned)at < (unsigned)rot.max_positions);
-      if (ok) {
-        float x[32];
-        const T* row = (const T*)in.k + (size_t)src * in.k_stride + h * D;
-        if (rot.table)
-          load32_turned<T>(row, j * 32, rot.table + (size_t)at * rot.rotary, rot, x);
-        else
-          load32<T>(row + j * 32, x);
-        const int byte = scale_byte(largest(x), kKeyScaleMin, kKeyScaleMax);
-        const uint4 c = codes_of<2, 1>(x, byte);
-        *reinterpret_cast<uint4*>(out.k + tile * (GP * D / 2) + t * (D / 2) + j * 16) = c;
-        scales[t * J + j] = (uint8_t)byte;
-        // the numbers that now stand for the key, for the page's bounds
-        const float scale = power_of(byte);
-        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint4 n = make_uint4(codes_to_bf16<0>(w[k], scale), codes_to_bf16<1>(w[k], scale), codes_to_bf16<2>(w[k], scale),
-                                     codes_to_bf16<3>(w[k], scale));
-          uint4* dst = reinterpret_cast<uint4*>(&lds[wave][t * D + j * 32 + 8 * k]);
-          if constexpr (sizeof(T) == 2) {
-            dst[0] = n;
-          } else {
-            dst[0] = make_uint4(n.x << 16, n.x & 0xFFFF0000u, n.y << 16, n.y & 0xFFFF0000u);
-            dst[1] = make_uint4(n.z << 16, n.z & 0xFFFF0000u, n.w << 16, n.w & 0xFFFF0000u);
-          }
+      for (int k = 0; k < 4; ++k) {
+        const uint4 n = make_uint4(codes_to_bf16<0>(w[k], scale), codes_to_bf16<1>(w[k], scale), codes_to_bf16<2>(w[k], scale),
+                                   codes_to_bf16<3>(w[k], scale));
+        uint4* dst = reinterpret_cast<uint4*>(&keys[hl][t * D + j * 32 + 8 * k]);
+        if constexpr (sizeof(T) == 2) {
+          dst[0] = n;
+        } else {
+          dst[0] = make_uint4(n.x << 16, n.x & 0xFFFF0000u, n.y << 16, n.y & 0xFFFF0000u);
+          dst[1] = make_uint4(n.z << 16, n.z & 0xFFFF0000u, n.w << 16, n.w & 0xFFFF0000u);
         }
-        load32<T>((const T*)in.v + (size_t)src * in.v_stride + h * D + j * 32, x);
-        const int vbyte = scale_byte(largest(x), kValueScaleMin, kValueScaleMax);
-        const uint4 vc = codes_of<1, 16>(x, vbyte);
-        scales[GP * J + t * J + j] = (uint8_t)vbyte;
-        const uint32_t vw[4] = {vc.x, vc.y, vc.z, vc.w};
-        uint8_t* dst = vcodes + ((t >> 2) * 16 * J + j) * 4 + (t & 3);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dst[r * J * 4] = (uint8_t)(vw[r / 4] >> (8 * (r % 4)));
       }
-      const unsigned long long who = __ballot(ok);
+    }
+  }
+  widen32<T>(vraw, x);
+  const int vbyte = scale_byte(largest(x), kValueScaleMin, kValueScaleMax);
+  const uint4 vc = codes_of<1, 16>(x, vbyte);
+  const uint32_t vw[4] = {vc.x, vc.y, vc.z, vc.w};
+  if (ok) scales[GP * J + t * J + j] = (uint8_t)vbyte;
+  const unsigned long long who = __ballot(ok);
+  const unsigned long long all = TPP * J == 64 ? ~0ull : (1ull << (TPP * J % 64)) - 1;
+  const int place = ((row >> 2) * 16 * J + j) * 4 + (row & 3);   // of byte 0 among this wavefront's bytes; byte r is r J 4 further
+  if (who == all) {   // every byte of this wavefront's rows: in order by way of LDS
+    if (row < TPP) {
 #pragma unroll
-      for (int i = 0; i < TPP; ++i) there |= (uint32_t)((who >> (i * J)) & 1) << (pass * TPP + i);
+      for (int r = 0; r < 16; ++r) codes[wave][place + r * J * 4] = (uint8_t)(vw[r / 4] >> (8 * (r % 4)));
     }
     wave_lds_fence();
-    if (kv.meta) bounds_from_lds<T, D>(lds[wave], there, f.lo, f.hi, f.lo > 0, (T*)kv.meta + tile * 2 * D, lane);
-    wave_lds_fence();   // the next head's keys go where this one's bounds were read
+    if (lane < TPP * D / 32)
+      *reinterpret_cast<uint4*>(vcodes + pass * (TPP * D / 2) + lane * 16) = *reinterpret_cast<const uint4*>(&codes[wave][lane * 16]);
+  } else if (ok) {
+    uint8_t* const dst = vcodes + pass * (TPP * D / 2) + place;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dst[r * J * 4] = (uint8_t)(vw[r / 4] >> (8 * (r % 4)));
   }
+  if (!kv.meta) return;
+  uint32_t there = 0;   // rows that hold a token now
+#pragma unroll
+  for (int i = 0; i < TPP; ++i) there |= (uint32_t)((who >> (i * J)) & 1) << (pass * TPP + i);
+  if constexpr (Work::PASSES == 1) {
+    wave_lds_fence();
+  } else {
+    if (lane == 0) arrived[wave] = there;
+    __syncthreads();
+    there = arrived[hl * 2] | arrived[hl * 2 + 1];
+    if (pass) return;
+  }
+  if (h < sh.Hkv) bounds_from_lds<T, D>(keys[hl], there, f.lo, f.hi, f.lo > 0, (T*)kv.meta + tile * 2 * D, lane);
 }
 
-// 32 numbers, as dwords of two bfloat16 each, to a row of T.
-template <typename T>
-__device__ __forceinline__ void store32(T* dst, const uint32_t (&w)[16]) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint4* to = reinterpret_cast<uint4*>(dst + 8 * k);
-    if constexpr (sizeof(T) == 2) {
-      to[0] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-    } else {
-      to[0] = make_uint4(w[4 * k] << 16, w[4 * k] & 0xFFFF0000u, w[4 * k + 1] << 16, w[4 * k + 1] & 0xFFFF0000u);
-      to[1] = make_uint4(w[4 * k + 2] << 16, w[4 * k + 2] & 0xFFFF0000u, w[4 * k + 3] << 16, w[4 * k + 3] & 0xFFFF0000u);
-    }
-  }
+// Eight numbers, as dwords of two bfloat16 each, to a row of T.
+__device__ __forceinline__ void store8(bf16_t* dst, const uint4& n) { *reinterpret_cast<uint4*>(dst) = n; }
+__device__ __forceinline__ void store8(float* dst, const uint4& n) {
+  reinterpret_cast<uint4*>(dst)[0] = make_uint4(n.x << 16, n.x & 0xFFFF0000u, n.y << 16, n.y & 0xFFFF0000u);
+  reinterpret_cast<uint4*>(dst)[1] = make_uint4(n.z << 16, n.z & 0xFFFF0000u, n.w << 16, n.w & 0xFFFF0000u);
 }
 
 template <typename T, int D, int GP>
 __global__ __launch_bounds__(256) void read_packed_kernel(KvView kv, Shape sh, const int32_t* indptr, int num_tokens, PackedView in,
                                                           T* __restrict__ k_out, T* __restrict__ v_out) {
-  constexpr int J = D / 32, TPP = 64 / J < GP ? 64 / J : GP;
+  constexpr int J = D / 32, LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, kTile = GP * D / 2;   // lanes per token, tokens per step of 16
+  constexpr int HALVES = GP / 16, HEADS = 4 / HALVES;
+  __shared__ __attribute__((aligned(16))) uint8_t codes[4][16 * D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = wave % HALVES, h = blockIdx.z * HEADS + wave / HALVES;
   const Fill f = fill_of(kv, sh, indptr, num_tokens, blockIdx.y, blockIdx.x);
-  if (f.hi <= f.lo) return;
-  const int j = lane % J;
-  for (int h = wave; h < sh.Hkv; h += 4) {
-    const size_t tile = (size_t)f.phys * sh.Hkv + h;
-    const uint8_t* scales = in.scales + tile * (2 * GP * J);
+  if (f.hi <= f.lo || h >= sh.Hkv || f.hi <= 16 * part || f.lo >= 16 * part + 16) return;
+  const int phys = kv.page_indices[f.entry];
+  if ((unsigned)phys >= (unsigned)kv.num_pages) return;
+  const size_t tile = (size_t)phys * sh.Hkv + h;
+  const uint8_t* const scales = in.scales + tile * (2 * GP * J) + 16 * part * J;
+  const int row = lane / LPT, c8 = lane % LPT, j = c8 / 4;   // this lane's token of a step, its eight channels, their group
+  // everything that is read, of the whole half page
+  uint32_t kc[STEPS];
+  uint8_t ks[STEPS], vs[STEPS];
+  uint4 vc = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-    for (int pass = 0; pass < GP / TPP; ++pass) {
-      const int t = pass * TPP + lane / J;
-      if (t < f.lo || t >= f.hi) continue;
-      const size_t row = ((size_t)(f.source + (t - f.lo)) * sh.Hkv + h) * D + j * 32;
-      uint32_t w[16];
-      if (k_out) {
-        const uint4 c = *reinterpret_cast<const uint4*>(in.k + tile * (GP * D / 2) + t * (D / 2) + j * 16);
-        const float scale = power_of(scales[t * J + j]);
-        const uint32_t cw[4] = {c.x, c.y, c.z, c.w};
+  for (int i = 0; i < STEPS; ++i) {
+    kc[i] = *reinterpret_cast<const uint32_t*>(in.k + tile * kTile + (16 * part + i * TPS + row) * (D / 2) + c8 * 4);
+    ks[i] = scales[(i * TPS + row) * J + j];
+    vs[i] = scales[GP * J + (i * TPS + row) * J + j];
+  }
+  if (lane < D / 2) vc = *reinterpret_cast<const uint4*>(in.v + tile * kTile + part * (8 * D) + lane * 16);
+  if (lane < D / 2) *reinterpret_cast<uint4*>(&codes[wave][lane * 16]) = vc;
+  wave_lds_fence();
+  const uint32_t pick = (c8 & 2) ? 0x07060302u : 0x05040100u;   // the second half of a group's channels are the high codes
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          w[4 * k] = codes_to_bf16<0>(cw[k], scale);
-          w[4 * k + 1] = codes_to_bf16<1>(cw[k], scale);
-          w[4 * k + 2] = codes_to_bf16<2>(cw[k], scale);
-          w[4 * k + 3] = codes_to_bf16<3>(cw[k], scale);
-        }
-        store32<T>(k_out + row, w);
-      }
-      if (v_out) {
-        const uint8_t* src = in.v + tile * (GP * D / 2) + ((t >> 2) * 16 * J + j) * 4 + (t & 3);
-        const float scale = power_of(scales[GP * J + t * J + j]);
-        uint32_t n[16];
+  for (int i = 0; i < STEPS; ++i) {
+    const int t = i * TPS + row, slot = 16 * part + t;
+    const size_t to = ((size_t)(f.source + (slot - f.lo)) * sh.Hkv + h) * D + c8 * 8;
+    const bool ok = slot >= f.lo && slot < f.hi;
+    if (k_out && ok) {
+      const float scale = power_of(ks[i]);
+      store8(k_out + to, make_uint4(codes_to_bf16<0>(kc[i], scale), codes_to_bf16<1>(kc[i], scale), codes_to_bf16<2>(kc[i], scale),
+                                    codes_to_bf16<3>(kc[i], scale)));
+    }
+    if (v_out && ok) {
+      const float scale = power_of(vs[i]);
+      const uint8_t* const from = &codes[wave][(((t >> 2) * 16 + (c8 & 1) * 8) * J + j) * 4 + (t & 3)];
+      uint32_t n[8];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) n[r] = src[r * J * 4];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) n[r] = codes_to_bf16<0>(n[r], scale);   // channels r and 16 + r
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          w[r / 2] = __builtin_amdgcn_perm(n[r + 1], n[r], 0x05040100u);
-          w[8 + r / 2] = __builtin_amdgcn_perm(n[r + 1], n[r], 0x07060302u);
-        }
-        store32<T>(v_out + row, w);
-      }
+      for (int r = 0; r < 8; ++r) n[r] = codes_to_bf16<0>(from[r * J * 4], scale);
+      store8(v_out + to, make_uint4(__builtin_amdgcn_perm(n[1], n[0], pick), __builtin_amdgcn_perm(n[3], n[2], pick),
+                                    __builtin_amdgcn_perm(n[5], n[4], pick), __builtin_amdgcn_perm(n[7], n[6], pick)));
     }
   }
 }
@@ -229,7 +284,8 @@ __global__ __launch_bounds__(256) void read_packed_kernel(KvView kv, Shape sh, c
 
 hipError_t launch_append_packed(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_new, const NewTokens& in,
                                 const Rotation& rot, const PackedView& out) {
-  const dim3 grid(pages_touched(max_new, sh.g), batch);
+  const int per_group = sh.g == 32 && sh.d == 128 ? 2 : 4;   // (PageWork::HEADS)
+  const dim3 grid(pages_touched(max_new, sh.g), batch, (sh.Hkv + per_group - 1) / per_group);
   auto launch = [&](auto kern) {
     kern<<<grid, 256, 0, st>>>(kv, sh, in, rot, out);
     return hipGetLastError();
@@ -242,7 +298,8 @@ static T* typed(void* p) { return static_cast<T*>(p); }
 
 hipError_t launch_read_packed(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_tokens, const int32_t* indptr,
                               int num_tokens, const PackedView& in, void* k_out, void* v_out) {
-  const dim3 grid(pages_touched(max_tokens, sh.g), batch);
+  const int per_group = sh.g == 32 ? 2 : 4;
+  const dim3 grid(pages_touched(max_tokens, sh.g), batch, (sh.Hkv + per_group - 1) / per_group);
   auto go = [&](auto kern, auto* k, auto* v) {
     kern<<<grid, 256, 0, st>>>(kv, sh, indptr, num_tokens, in, k, v);
     return hipGetLastError();
