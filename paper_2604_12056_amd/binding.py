@@ -175,8 +175,10 @@ class PackedKV:
         self.max_seq_pages = int(max_seq_pages)
 
     def as_struct(self) -> losa_packed_kv:
-        return losa_packed_kv(_ptr(self.k_codes), _ptr(self.v_codes), _ptr(self.scales), _ptr(self.meta), _ptr(self.page_indptr),
-                              _ptr(self.page_indices), _ptr(self.seq_lens), self.batch, self.num_pages, self.max_seq_pages)
+        meta = self.meta
+        return losa_packed_kv(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.scales.data_ptr(),
+                              None if meta is None else meta.data_ptr(), self.page_indptr.data_ptr(), self.page_indices.data_ptr(),
+                              self.seq_lens.data_ptr(), self.batch, self.num_pages, self.max_seq_pages)
 
     def for_scoring(self) -> PagedKV:
         """The cache as losa_score_pages and losa_score_pages_shared take it: they read its page table and bounds only."""
@@ -312,6 +314,8 @@ def _row_stride(t, ctx: Context, tokens: int, heads: int, what: str) -> int:
         raise LosaError(LOSA_ERR_INVALID_ARG, f"{what} is not a [{tokens}, {heads}, {d}] tensor of the context's type")
     if tokens == 0:
         return 0
+    if t.is_contiguous():
+        return heads * d if tokens > 1 else 0
     row, head, channel = t.stride()
     if channel != 1 or (head != d and heads > 1):
         raise LosaError(LOSA_ERR_INVALID_ARG, f"{what}: the heads of a token do not lie one behind the other")
@@ -366,10 +370,11 @@ def losa_read_packed(ctx: Context, kv: PackedKV, tok_indptr, k_out, v_out, max_t
     """The last tokens of every sequence of a 4-bit cache into k_out / v_out [tokens, Hkv, d] (contiguous; either may be None)."""
     one = k_out if k_out is not None else v_out
     n = 0 if one is None else one.shape[0]
+    shape = (n, ctx.kv_heads, ctx.head_dim)
     for t in (k_out, v_out):
-        if t is not None and _row_stride(t, ctx, n, ctx.kv_heads, "an output") not in (0, ctx.kv_heads * ctx.head_dim):
-            raise LosaError(LOSA_ERR_INVALID_ARG, "outputs are contiguous")
-    _check(ctx, load_library().losa_read_packed(ctx.handle, _stream(stream), C.byref(kv.as_struct()), _ptr(tok_indptr), n, max_tokens,
+        if t is not None and (t.shape != shape or t.element_size() != ctx.element_size or not t.is_contiguous()):
+            raise LosaError(LOSA_ERR_INVALID_ARG, f"an output is not a contiguous {list(shape)} tensor of the context's type")
+    _check(ctx, load_library().losa_read_packed(ctx.handle, _stream(stream), C.byref(kv.as_struct()), tok_indptr.data_ptr(), n, max_tokens,
                                                _ptr(k_out), _ptr(v_out)))
 
 

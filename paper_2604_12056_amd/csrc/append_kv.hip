@@ -7,15 +7,14 @@
 
 namespace losa {
 
-// ---- rotation alone.  A thread has one unit (two 16-byte chunks) of HPT heads of a token: the angles are read once for them,
-// and the loads of all heads leave together.
+// ---- rotation alone.  A thread has one unit (two 16-byte chunks) of a head of a token.
 struct RotateSide {
   const void* x;
   void* y;
   long x_stride, y_stride;
   int heads;
 };
-template <typename T, int HPT>
+template <typename T>
 __global__ __launch_bounds__(256) void rotate_kernel(Rotation rot, const int32_t* __restrict__ positions, int tokens, int d, RotateSide q,
                                                      RotateSide k) {
   constexpr int V = Vec16<T>::n;
@@ -24,36 +23,24 @@ __global__ __launch_bounds__(256) void rotate_kernel(Rotation rot, const int32_t
   const long t = item / units;
   const Unit u = unit_of<V>((int)(item % units), rot.rotary, rot.pairs);
   if (t >= tokens) return;
-  const int at = positions[t], head0 = blockIdx.y * HPT, heads = q.heads + k.heads;
-  uint4 a[HPT], b[HPT];
-#pragma unroll
-  for (int i = 0; i < HPT; ++i) {
-    const int h = min(head0 + i, heads - 1);
-    const T* row = h < q.heads ? (const T*)q.x + t * q.x_stride + h * d : (const T*)k.x + t * k.x_stride + (h - q.heads) * d;
-    a[i] = *reinterpret_cast<const uint4*>(row + u.first);
-    b[i] = *reinterpret_cast<const uint4*>(row + u.second);
-  }
+  const int at = positions[t], h = blockIdx.y;
+  const T* from = h < q.heads ? (const T*)q.x + t * q.x_stride + h * d : (const T*)k.x + t * k.x_stride + (h - q.heads) * d;
+  uint4 a = *reinterpret_cast<const uint4*>(from + u.first), b = *reinterpret_cast<const uint4*>(from + u.second);
   if ((unsigned)at >= (unsigned)rot.max_positions) return;
-  float c[V], s[V];
-  const float* angles = rot.table + (size_t)at * rot.rotary + max(u.angle, 0);
-  load_floats<V>(angles, c);
-  load_floats<V>(angles + rot.rotary / 2, s);
-#pragma unroll
-  for (int i = 0; i < HPT; ++i) {
-    const int h = head0 + i;
-    if (h >= heads) return;
-    if (u.angle >= 0) {
-      float fa[V], fb[V];
-      widen16(a[i], fa, T());
-      widen16(b[i], fb, T());
-      turn_unit<V>(fa, fb, c, s, rot.pairs);
-      a[i] = round16(fa, T());
-      b[i] = round16(fb, T());
-    }
-    T* row = h < q.heads ? (T*)q.y + t * q.y_stride + h * d : (T*)k.y + t * k.y_stride + (h - q.heads) * d;
-    *reinterpret_cast<uint4*>(row + u.first) = a[i];
-    *reinterpret_cast<uint4*>(row + u.second) = b[i];
+  if (u.angle >= 0) {
+    float c[V], s[V], fa[V], fb[V];
+    const float* angles = rot.table + (size_t)at * rot.rotary + u.angle;
+    load_floats<V>(angles, c);
+    load_floats<V>(angles + rot.rotary / 2, s);
+    widen16(a, fa, T());
+    widen16(b, fb, T());
+    turn_unit<V>(fa, fb, c, s, rot.pairs);
+    a = round16(fa, T());
+    b = round16(fb, T());
   }
+  T* to = h < q.heads ? (T*)q.y + t * q.y_stride + h * d : (T*)k.y + t * k.y_stride + (h - q.heads) * d;
+  *reinterpret_cast<uint4*>(to + u.first) = a;
+  *reinterpret_cast<uint4*>(to + u.second) = b;
 }
 
 template <typename T>
@@ -62,7 +49,7 @@ static hipError_t launch_rotate_t(hipStream_t st, int d, const Rotation& rot, co
   const long items = (long)tokens * (d / (2 * Vec16<T>::n));
   const int heads = q.heads + k.heads;
   const unsigned groups = (unsigned)((items + 255) / 256);
-  rotate_kernel<T, 1><<<dim3(groups, heads), 256, 0, st>>>(rot, positions, tokens, d, q, k);
+  rotate_kernel<T><<<dim3(groups, heads), 256, 0, st>>>(rot, positions, tokens, d, q, k);
   return hipGetLastError();
 }
 
@@ -74,7 +61,8 @@ hipError_t launch_rotate(hipStream_t st, int dtype, int d, const Rotation& rot, 
                             : launch_rotate_t<float>(st, d, rot, positions, tokens, qs, ks);
 }
 
-// ---- new tokens into pages.  A workgroup fills one page, each of its four wavefronts every fourth KV head of it.
+// ---- new tokens into pages.  A wavefront has 16 tokens of a page and KV head, a workgroup four of them: a page of four heads, or of two
+// where a page has 32 tokens.  All of a wavefront's reads leave before it uses any.
 //
 // Keys: d / (2 V) lanes per token, a unit each, turned where there is a rotation, written as they lie (token-major) and left in
 // LDS, out of which a lane takes the bounds of its channels.
@@ -83,109 +71,137 @@ hipError_t launch_rotate(hipStream_t st, int dtype, int d, const Rotation& rot, 
 // LDS and no lane exchange.  Rows that get no token are not written.
 template <typename T, int D, int GP>
 __global__ __launch_bounds__(256) void append_kernel(KvView kv, Shape sh, NewTokens in, Rotation rot) {
-  constexpr int V = Vec16<T>::n, LPT = D / (2 * V), TPP = 64 / LPT;   // lanes per token, tokens per pass
-  __shared__ __attribute__((aligned(16))) T lds[4][GP * D];
+  constexpr int V = Vec16<T>::n, LPT = D / (2 * V), TPP = 64 / LPT, PASSES = 16 / TPP;   // keys: lanes per token, tokens per pass
+  constexpr int HALVES = GP / 16, HEADS = 4 / HALVES;
+  constexpr int E = 4 / sizeof(T), WPT = D / E, LPR = WPT < 64 ? WPT : 64;   // values: channels of a dword, dwords and lanes per token
+  constexpr int SETS = 64 / LPR, OCTETS = 2 / SETS, COLS = WPT / LPR;        // octets of tokens side by side, one after the other; dwords of a lane per token
+  __shared__ __attribute__((aligned(16))) T lds[HEADS][GP * D];
+  __shared__ uint32_t arrived[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = wave % HALVES, hl = wave / HALVES, h = blockIdx.z * HEADS + hl, head = min(h, sh.Hkv - 1);
   const Fill f = fill_of(kv, sh, in.indptr, in.num_tokens, blockIdx.y, blockIdx.x);
   if (f.hi <= f.lo) return;
   const int phys = kv.page_indices[f.entry];
-  if ((unsigned)phys >= (unsigned)kv.num_pages) return;
   const Unit u = unit_of<V>(lane % LPT, rot.table ? rot.rotary : 0, rot.pairs);
-  for (int j = wave; j < sh.Hkv; j += 4) {
-    const size_t tile = (size_t)phys * sh.Hkv + j;
-    uint32_t there = 0;   // rows that hold a token now
-    T* rows = lds[wave];
-#pragma unroll
-    for (int pass = 0; pass < GP / TPP; ++pass) {
-      const int t = pass * TPP + lane / LPT;
-      const bool mine = t >= f.lo && t < f.hi;
-      const int src = f.source + (t - f.lo);
-      int at = 0;
-      if (mine && rot.table) at = in.positions ? in.positions[src] : f.slot + (t - f.lo);
-      const bool ok = mine && (!rot.table || (unsigned)at < (unsigned)rot.max_positions);
-      if (ok) {
-        const T* row = (const T*)in.k + (size_t)src * in.k_stride + j * D;
-        uint4 a = *reinterpret_cast<const uint4*>(row + u.first), b = *reinterpret_cast<const uint4*>(row + u.second);
-        if (u.angle >= 0) {
-          float fa[V], fb[V], c[V], s[V];
-          const float* angles = rot.table + (size_t)at * rot.rotary + u.angle;
-          load_floats<V>(angles, c);
-          load_floats<V>(angles + rot.rotary / 2, s);
-          widen16(a, fa, T());
-          widen16(b, fb, T());
-          turn_unit<V>(fa, fb, c, s, rot.pairs);
-          a = round16(fa, T());
-          b = round16(fb, T());
-        }
-        T* dst = (T*)kv.k_pages + tile * (GP * D) + t * D;
-        *reinterpret_cast<uint4*>(dst + u.first) = a;
-        *reinterpret_cast<uint4*>(dst + u.second) = b;
-        *reinterpret_cast<uint4*>(rows + t * D + u.first) = a;
-        *reinterpret_cast<uint4*>(rows + t * D + u.second) = b;
-      }
-      const unsigned long long who = __ballot(ok);
-#pragma unroll
-      for (int i = 0; i < TPP; ++i) there |= (uint32_t)((who >> (i * LPT)) & 1) << (pass * TPP + i);
-    }
-    wave_lds_fence();
-    if (kv.meta) bounds_from_lds<T, D>(rows, there, f.lo, f.hi, f.lo > 0, (T*)kv.meta + tile * 2 * D, lane);
 
-    // values: E channels of a lane, eight tokens a time
-    constexpr int E = 4 / sizeof(T), WPT = D / E;   // dwords per token
-    constexpr int SETS = WPT >= 64 ? 1 : 64 / WPT;  // octets of tokens side by side
-    const T* vrow = (const T*)in.v + (size_t)f.source * in.v_stride + j * D;
-    T* vpage = (T*)kv.v_pages + tile * (GP * D);
-    for (int w = 0; w < WPT; w += 64) {
-      const int at = WPT >= 64 ? w + lane : lane % WPT;
+  // reads: rows that are not there read one that is
+  const int most = f.hi - f.lo - 1;
+  uint4 a[PASSES], b[PASSES];
+  int row[PASSES];
+  bool ok[PASSES];
 #pragma unroll
-      for (int o = 0; o < GP / 8; o += SETS) {
-        const int t0 = 8 * (o + (WPT >= 64 ? 0 : lane / WPT));
-        const uint32_t mask = (there >> t0) & 0xFFu;
-        uint32_t x[8];
+  for (int i = 0; i < PASSES; ++i) {
+    row[i] = 16 * half + i * TPP + lane / LPT;
+    ok[i] = row[i] >= f.lo && row[i] < f.hi && h < sh.Hkv;
+    const T* from = (const T*)in.k + (size_t)(f.source + max(0, min(row[i] - f.lo, most))) * in.k_stride + head * D;
+    a[i] = *reinterpret_cast<const uint4*>(from + u.first);
+    b[i] = *reinterpret_cast<const uint4*>(from + u.second);
+  }
+  const int col = lane % LPR, set = lane / LPR;
+  uint32_t x[OCTETS][COLS][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          x[i] = ((mask >> i) & 1) ? reinterpret_cast<const uint32_t*>(vrow + (long)(t0 + i - f.lo) * in.v_stride)[at] : 0u;
+  for (int o = 0; o < OCTETS; ++o)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int t = 16 * half + 8 * (o * SETS + set) + e;
+      const T* from = (const T*)in.v + (size_t)(f.source + max(0, min(t - f.lo, most))) * in.v_stride + head * D;
+#pragma unroll
+      for (int w = 0; w < COLS; ++w) x[o][w][e] = reinterpret_cast<const uint32_t*>(from)[w * 64 + col];
+    }
+  float c[PASSES][V], s[PASSES][V];
+  if (rot.table) {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int new_row = max(0, min(row[i] - f.lo, most));
+      const int at = in.positions ? in.positions[f.source + new_row] : f.slot + new_row;
+      const bool known = (unsigned)at < (unsigned)rot.max_positions;
+      ok[i] = ok[i] && known;
+      const float* angles = rot.table + (size_t)(known ? at : 0) * rot.rotary + max(u.angle, 0);
+      load_floats<V>(angles, c[i]);
+      load_floats<V>(angles + rot.rotary / 2, s[i]);
+    }
+  }
+  if ((unsigned)phys >= (unsigned)kv.num_pages) return;
+  const size_t tile = (size_t)phys * sh.Hkv + head;
+
+  uint32_t there = 0;   // rows of these 16 that hold a token now
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    if (rot.table && u.angle >= 0) {
+      float fa[V], fb[V];
+      widen16(a[i], fa, T());
+      widen16(b[i], fb, T());
+      turn_unit<V>(fa, fb, c[i], s[i], rot.pairs);
+      a[i] = round16(fa, T());
+      b[i] = round16(fb, T());
+    }
+    if (ok[i]) {
+      T* dst = (T*)kv.k_pages + tile * (GP * D) + row[i] * D;
+      *reinterpret_cast<uint4*>(dst + u.first) = a[i];
+      *reinterpret_cast<uint4*>(dst + u.second) = b[i];
+      if (kv.meta) {
+        *reinterpret_cast<uint4*>(lds[hl] + row[i] * D + u.first) = a[i];
+        *reinterpret_cast<uint4*>(lds[hl] + row[i] * D + u.second) = b[i];
+      }
+    }
+    const unsigned long long who = __ballot(ok[i]);
+#pragma unroll
+    for (int t = 0; t < TPP; ++t) there |= (uint32_t)((who >> (t * LPT)) & 1) << (i * TPP + t);
+  }
+
+  T* vpage = (T*)kv.v_pages + tile * (GP * D) + 16 * half;
+#pragma unroll
+  for (int o = 0; o < OCTETS; ++o) {
+    const int t0 = 8 * (o * SETS + set);
+    const uint32_t mask = (there >> t0) & 0xFFu;
+#pragma unroll
+    for (int w = 0; w < COLS; ++w) {
+      const uint32_t(&y)[8] = x[o][w];
+      T* dst = vpage + (w * 64 + col) * E * GP + t0;
+      if (mask == 0xFFu) {
         if constexpr (E == 2) {
-          if (mask == 0xFFu) {
-            uint4 lo, hi;
-            lo.x = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
-            lo.y = __builtin_amdgcn_perm(x[3], x[2], 0x05040100u);
-            lo.z = __builtin_amdgcn_perm(x[5], x[4], 0x05040100u);
-            lo.w = __builtin_amdgcn_perm(x[7], x[6], 0x05040100u);
-            hi.x = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
-            hi.y = __builtin_amdgcn_perm(x[3], x[2], 0x07060302u);
-            hi.z = __builtin_amdgcn_perm(x[5], x[4], 0x07060302u);
-            hi.w = __builtin_amdgcn_perm(x[7], x[6], 0x07060302u);
-            *reinterpret_cast<uint4*>(vpage + (2 * at) * GP + t0) = lo;
-            *reinterpret_cast<uint4*>(vpage + (2 * at + 1) * GP + t0) = hi;
-          } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if ((mask >> i) & 1) {
-                vpage[(2 * at) * GP + t0 + i] = (T)(x[i] & 0xFFFFu);
-                vpage[(2 * at + 1) * GP + t0 + i] = (T)(x[i] >> 16);
-              }
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t pick = e ? 0x07060302u : 0x05040100u;
+            *reinterpret_cast<uint4*>(dst + e * GP) =
+                make_uint4(__builtin_amdgcn_perm(y[1], y[0], pick), __builtin_amdgcn_perm(y[3], y[2], pick), __builtin_amdgcn_perm(y[5], y[4], pick),
+                           __builtin_amdgcn_perm(y[7], y[6], pick));
           }
         } else {
-          if (mask == 0xFFu) {
-            uint4* dst = reinterpret_cast<uint4*>(vpage + at * GP + t0);
-            dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
-            dst[1] = make_uint4(x[4], x[5], x[6], x[7]);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if ((mask >> i) & 1) reinterpret_cast<uint32_t*>(vpage)[at * GP + t0 + i] = x[i];
-          }
+          reinterpret_cast<uint4*>(dst)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+          reinterpret_cast<uint4*>(dst)[1] = make_uint4(y[4], y[5], y[6], y[7]);
         }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if ((mask >> e) & 1) {
+            if constexpr (E == 2) {
+              dst[e] = (T)(y[e] & 0xFFFFu);
+              dst[GP + e] = (T)(y[e] >> 16);
+            } else {
+              reinterpret_cast<uint32_t*>(dst)[e] = y[e];
+            }
+          }
       }
     }
-    wave_lds_fence();   // the next head's keys go where this one's bounds were read
   }
+  if (!kv.meta) return;
+  there <<= 16 * half;
+  if constexpr (HALVES == 1) {
+    wave_lds_fence();
+  } else {
+    if (lane == 0) arrived[wave] = there;
+    __syncthreads();
+    there = arrived[hl * 2] | arrived[hl * 2 + 1];
+    if (half) return;
+  }
+  if (h < sh.Hkv) bounds_from_lds<T, D>(lds[hl], there, f.lo, f.hi, f.lo > 0, (T*)kv.meta + tile * 2 * D, lane);
 }
 
 hipError_t launch_append(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_new, const NewTokens& in,
                          const Rotation& rot) {
-  const dim3 grid(pages_touched(max_new, sh.g), batch);
+  const int per_group = sh.g == 32 ? 2 : 4;
+  const dim3 grid(pages_touched(max_new, sh.g), batch, (sh.Hkv + per_group - 1) / per_group);
   auto launch = [&](auto kern) {
     kern<<<grid, 256, 0, st>>>(kv, sh, in, rot);
     return hipGetLastError();

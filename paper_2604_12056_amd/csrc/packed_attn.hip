@@ -39,6 +39,10 @@ __device__ __forceinline__ float over_lane_groups_max(float v) {
   return __uint_as_float(across_rows(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
 }
 
+__device__ __forceinline__ float over_lane_groups_sum(float v) {
+  return __uint_as_float(across_rows(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+
 // 16 or 8 bytes of codes per lane, as dwords
 template <int N>
 __device__ __forceinline__ void load_dwords(const uint8_t* p, uint32_t (&w)[N]) {
@@ -125,19 +129,24 @@ __device__ __forceinline__ float remainder_of(float p, f16x2_t hi) {
   return r;
 }
 
-// Numerators of a lane's four tokens of two subtiles as pairs of halves.
+// Numerators of two neighbouring scores as pairs of halves, element e and the next of the operands; their sum.
+__device__ __forceinline__ float numerator_pair(float s0, float s1, float scale_log2e, float neg_m, int e, f16x8_t& p_hi, f16x8_t& p_lo) {
+  const f32x2_t p = {__builtin_amdgcn_exp2f(fmaf(s0, scale_log2e, neg_m)), __builtin_amdgcn_exp2f(fmaf(s1, scale_log2e, neg_m))};
+  const f16x2_t hi = __builtin_convertvector(p, f16x2_t);
+  const f32x2_t rest = {remainder_of<false>(p[0], hi), remainder_of<true>(p[1], hi)};
+  const f16x2_t lo = __builtin_convertvector(rest, f16x2_t);
+  p_hi[e] = hi[0];
+  p_hi[e + 1] = hi[1];
+  p_lo[e] = lo[0];
+  p_lo[e + 1] = lo[1];
+  return p[0] + p[1];
+}
+// ... of a lane's four tokens of two subtiles.
 __device__ __forceinline__ void numerators(const f32x4_t& a, const f32x4_t& b, float scale_log2e, float neg_m, f16x8_t& p_hi, f16x8_t& p_lo) {
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const f32x4_t& s = e < 4 ? a : b;
-    const f32x2_t p = {__builtin_amdgcn_exp2f(fmaf(s[e & 3], scale_log2e, neg_m)), __builtin_amdgcn_exp2f(fmaf(s[(e & 3) + 1], scale_log2e, neg_m))};
-    const f16x2_t hi = __builtin_convertvector(p, f16x2_t);
-    const f32x2_t rest = {remainder_of<false>(p[0], hi), remainder_of<true>(p[1], hi)};
-    const f16x2_t lo = __builtin_convertvector(rest, f16x2_t);
-    p_hi[e] = hi[0];
-    p_hi[e + 1] = hi[1];
-    p_lo[e] = lo[0];
-    p_lo[e + 1] = lo[1];
+    numerator_pair(s[e & 3], s[(e & 3) + 1], scale_log2e, neg_m, e, p_hi, p_lo);
   }
 }
 // One more row of values, all ones: its products with the numerators are their sums, on the matrix core, which has time for them where the vector
@@ -671,11 +680,34 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
 // ---- more than 64 query rows: the eight wavefronts of a workgroup have R*16 rows each and share the tiles.
 //
 // Two tiles of the workgroup's share are a stage of 64 tokens, four subtiles.  Every wavefront reads one subtile's codes, of keys or of values, converts
-// them once for all rows and leaves them in LDS as the matrix core's operands, 16 bytes a lane, in lane order.  Two LDS buffers and
-// a barrier per stage; the codes of the next kAhead stages are on their way in registers.
+// them once for all rows and leaves them in LDS as the matrix core's operands, 16 bytes a lane, in lane order.  A barrier per stage, two LDS buffers of
+// keys and three of values (see compute_stage); the codes of the next kAhead stages are on their way in registers.
+//
+// Bound by the matrix core: three products per useful two, the values' being with pairs of halves.  64 tokens' queries against four prefixes of 65536 (256 rows, 8 KV heads) take
+// 323 us, 1.28 PFLOP/s executed, which is what a large bfloat16 product of the library's reaches here.  Reading each operand, waiting for it and using it took
+// 413 us; scores, numerators and products one after the other, each for all of a stage, 371.
 template <int D>
-constexpr int kStageBytes = 64 * D * 2 * 2;   // keys, then values
+constexpr int kKeyBytes = 64 * D * 2;   // of a stage, and as many of values
+template <int D>
+constexpr int kStagedBytes = 5 * kKeyBytes<D>;
 constexpr int kAhead = 2;
+
+// use(n, operand) for operands 0 .. N-1, 16 bytes a lane and 1024 bytes apart in LDS, each read kReadsAhead uses before its own.  (Left to its own order,
+// the compiler reads one, waits for it and uses it.)
+constexpr int kReadsAhead = 2;
+template <typename V, int N, typename F>
+__device__ __forceinline__ void with_operands(const char* from, F&& use) {
+  V x[kReadsAhead + 1];
+#pragma unroll
+  for (int n = 0; n < kReadsAhead; ++n) x[n] = *reinterpret_cast<const V*>(from + n * 1024);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (n + kReadsAhead < N) x[(n + kReadsAhead) % (kReadsAhead + 1)] = *reinterpret_cast<const V*>(from + (n + kReadsAhead) * 1024);
+    __builtin_amdgcn_sched_barrier(0);
+    use(n, x[n % (kReadsAhead + 1)]);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 template <int D, int GP, int R>
 __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& sh, const AttnInputs& in, const PackedView& pk, const Segment& seg, int row_base,
@@ -724,32 +756,35 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
   struct Raw {
     uint32_t c[W], vs[4], ks;   // codes of keys or of values
   };
-  const bool has_keys = wave < 4;
+  // Of two wavefronts on a SIMD the older one has the way free, so the younger ones (4 .. 7) get the shorter conversions, and precedence: without
+  // either they were at work for 5400 cycles a stage, the others for 4000, of 5650.
+  const bool has_keys = wave >= 4;
+  if (has_keys) __builtin_amdgcn_s_setprio(1);
   const int mysub = wave & 3;
+  const uint32_t code_at = has_keys ? l16 * (D / 2) + qd * (CPL / 2) : (qd * 16 + l16) * (J * 4);   // (a tile's first 16 tokens)
+  const uint32_t key_scale_at = l16 * J + qd * CPL / 32, scales_at = GP * J + qd * 4 * J;
   auto load_stage = [&](Raw& x, int i) {   // (past the end: the pool's first page, as nothing depends on it)
     const int at = ((2 * i + mysub / 2) * PPT + (GP == 16 ? mysub % 2 : 0)) & 63;
     const size_t tile = (size_t)__builtin_amdgcn_readlane(pg_phys, at) * sh.Hkv + j;
     const int row = GP == 16 ? 0 : 16 * (mysub % 2);
-    const uint8_t* sc = pk.scales + tile * (2 * GP * J);
-    const uint8_t* keys = pk.k + tile * kTileBytes + (row + l16) * (D / 2) + qd * (CPL / 2);
-    const uint8_t* values = pk.v + tile * kTileBytes + ((row / 4 + qd) * 16 + l16) * (J * 4);
-    load_dwords<W>(has_keys ? keys : values, x.c);
-    x.ks = sc[(row + l16) * J + qd * CPL / 32];   // (one of the two in vain: no branch around a load)
-    load_scales<J>(sc + GP * J + (row + qd * 4) * J, x.vs);
+    const uint8_t* sc = pk.scales + tile * (2 * GP * J) + row * J;
+    load_dwords<W>((has_keys ? pk.k : pk.v) + tile * kTileBytes + row * (D / 2) + code_at, x.c);   // (16 tokens are as many bytes in either order)
+    x.ks = sc[key_scale_at];   // (one of the two in vain: no branch around a load)
+    load_scales<J>(sc + scales_at, x.vs);
   };
-  auto convert_stage = [&](Raw& x, int i, char* buf) {
+  auto convert_stage = [&](Raw& x, int i, char* keys, char* values) {
     if (has_keys) {
       const float scale = power_of(x.ks);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        *reinterpret_cast<uint4*>(buf + ((mysub * KS + ks) * 64 + lane) * 16) =
+        *reinterpret_cast<uint4*>(keys + ((mysub * KS + ks) * 64 + lane) * 16) =
             make_uint4(codes_to_bf16<0>(x.c[ks], scale), codes_to_bf16<1>(x.c[ks], scale), codes_to_bf16<2>(x.c[ks], scale), codes_to_bf16<3>(x.c[ks], scale));
     }
     if (!has_keys) {
       const int valid = valid_of(i, mysub);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.vs[e] = qd * 4 + e < valid ? x.vs[e] : 0u;   // (see the other form)
-      char* v = buf + 64 * D * 2 + ((mysub / 2) * NT * 64 + lane) * 16 + (mysub % 2) * 8;
+      char* v = values + ((mysub / 2) * NT * 64 + lane) * 16 + (mysub % 2) * 8;
 #pragma unroll
       for (int g = 0; g < J; ++g) {
         uint2 lo, hi;
@@ -760,32 +795,57 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     }
   };
 
-  float m_run[R], up_thr[R];
+  float m_run[R], up_thr[R], l_run[R];   // l_run: of this lane's tokens
   const float inv_scale_log2e = 1.0f / scale_log2e;
-  f32x4_t o[R][NT], l_sum[R];   // (a row's sum in all four components)
+  f32x4_t o[R][NT];
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) {
     m_run[mt] = kNegBig;
     up_thr[mt] = -INFINITY;
-    l_sum[mt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    l_run[mt] = 0.f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) o[mt][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   }
   const bool has_rows = row0 < M;   // (the others convert only)
 
-  auto compute_stage = [&](int i, const char* buf, bool first) {
-    f32x4_t sc[R][4];
+  // A stage: scores and their maxima, then for its two pairs of subtiles numerators and their products with the values.  The matrix core works on a pair's
+  // products while the vector units make the next pair's numerators, so the second pair's products come with the next stage's first numerators.
+  f32x4_t sc[R][4];
+  f16x8_t p_hi[2][R], p_lo[2][R];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+  for (int mt = 0; mt < R; ++mt)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p_hi[1][mt][e] = p_lo[1][mt][e] = (_Float16)0.f;   // (ahead of the first stage: nothing, times that stage's values)
+  char* values[3] = {lds + 2 * kKeyBytes<D>, lds + 3 * kKeyBytes<D>, lds + 4 * kKeyBytes<D>};   // the last stage's, this one's, the next one's
+  auto numerators_of = [&](int pair, int i) {   // scores 2 i' and 2 i' + 1, i' = i % 4, of row tile i / 4
+    const int mt = i / 4, e = 2 * (i % 4);
+    const f32x4_t& s = sc[mt][2 * pair + e / 4];
+    l_run[mt] += numerator_pair(s[e & 3], s[(e & 3) + 1], scale_log2e, -m_run[mt], e, p_hi[pair][mt], p_lo[pair][mt]);
+  };
+  auto products_of = [&](int pair, const char* from, auto&& beside) {   // beside(n) goes with channels 16 n and the next 15
+    with_operands<f16x8_t, NT>(from + (pair * NT * 64 + lane) * 16, [&](int n, const f16x8_t& vf) {
+#pragma unroll
+      for (int mt = 0; mt < R; ++mt) o[mt][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_hi[pair][mt], o[mt][n], 0, 0, 0);
+#pragma unroll
+      for (int mt = 0; mt < R; ++mt) o[mt][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_lo[pair][mt], o[mt][n], 0, 0, 0);
+      beside(n);
+    });
+  };
+  auto numerators_beside = [&](int pair) {
+    return [&, pair](int n) {
+#pragma unroll
+      for (int i = n * 4 * R / NT; i < (n + 1) * 4 * R / NT; ++i) numerators_of(pair, i);
+    };
+  };
+  auto compute_stage = [&](int i, const char* keys, const char* last_values) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) sc[mt][s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    with_operands<bf16x8_t, 4 * KS>(keys + lane * 16, [&](int n, const bf16x8_t& kf) {   // subtile n / KS, channels n % KS
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(buf + ((s * KS + ks) * 64 + lane) * 16);
-#pragma unroll
-        for (int mt = 0; mt < R; ++mt) sc[mt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][ks], sc[mt][s], 0, 0, 0);
-      }
-    }
+      for (int mt = 0; mt < R; ++mt) sc[mt][n / KS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][n % KS], sc[mt][n / KS], 0, 0, 0);
+    });
     int nv[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) nv[s] = valid_of(i, s);
@@ -808,38 +868,27 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
         for (int e = 0; e < 4; ++e) tm[mt] = fmaxf(tm[mt], sc[mt][s][e]);
       any_up |= tm[mt] > up_thr[mt];
     }
-    if (__any(any_up)) {
+    float alpha[R];
+    const bool rescale = __any(any_up);
+    if (rescale) {
 #pragma unroll
       for (int mt = 0; mt < R; ++mt) {
         const float cand = over_lane_groups_max(tm[mt]) * scale_log2e - kHeadroom;
         const bool up = cand > m_run[mt] + kLag;
-        const float alpha = up ? __builtin_amdgcn_exp2f(m_run[mt] - cand) : 1.0f;
+        alpha[mt] = up ? __builtin_amdgcn_exp2f(m_run[mt] - cand) : 1.0f;
         m_run[mt] = up ? cand : m_run[mt];
         up_thr[mt] = (m_run[mt] + kHeadroom + kLag) * inv_scale_log2e;
-        l_sum[mt] *= alpha;
-        if (!first) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) o[mt][nt] *= alpha;
-        }
+        l_run[mt] *= alpha[mt];
       }
     }
+    products_of(1, last_values, numerators_beside(0));
+    if (rescale) {   // (what was owed was against the old reference)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {   // a pair of subtiles at a time
-      f16x8_t p_hi[R], p_lo[R];
+      for (int mt = 0; mt < R; ++mt)
 #pragma unroll
-      for (int mt = 0; mt < R; ++mt) {
-        numerators(sc[mt][2 * h], sc[mt][2 * h + 1], scale_log2e, -m_run[mt], p_hi[mt], p_lo[mt]);
-        l_sum[mt] = sum_of(p_hi[mt], p_lo[mt], l_sum[mt]);
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const f16x8_t vf = *reinterpret_cast<const f16x8_t*>(buf + 64 * D * 2 + ((h * NT + nt) * 64 + lane) * 16);
-#pragma unroll
-        for (int mt = 0; mt < R; ++mt) o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_hi[mt], o[mt][nt], 0, 0, 0);
-#pragma unroll
-        for (int mt = 0; mt < R; ++mt) o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_lo[mt], o[mt][nt], 0, 0, 0);
-      }
+        for (int nt = 0; nt < NT; ++nt) o[mt][nt] *= alpha[mt];
     }
+    products_of(0, values[1], numerators_beside(1));
   };
 
   constexpr int SPF = TPR / 2;   // stages per fetch of page entries
@@ -850,28 +899,36 @@ __device__ __forceinline__ void packed_rows_body(const KvView& kv, const Shape& 
     if (n0 > 0) __syncthreads();            // the buffers' last readers are done
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) load_stage(raw[k], k);
-    convert_stage(raw[0], 0, lds);
+    convert_stage(raw[0], 0, lds, values[1]);
     load_stage(raw[0], kAhead);
     __syncthreads();
     for (int i = 0; i < ne; i += 2) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        // Stage i + k is in buffer k, the next one goes to the other.  (Whether there is one or not: loads behind a branch, or a use of theirs,
+        // Stage i + k's keys are in buffer k, the next one's go to the other.  (Whether there is one or not: loads behind a branch, or a use of theirs,
         // would be waited for where the branches join.)
-        convert_stage(raw[(k + 1) % kAhead], i + k + 1, lds + (1 - k) * kStageBytes<D>);
+        convert_stage(raw[(k + 1) % kAhead], i + k + 1, lds + (1 - k) * kKeyBytes<D>, values[2]);
         load_stage(raw[(k + 1) % kAhead], i + k + 1 + kAhead);
-        if (has_rows && i + k < ne) compute_stage(i + k, lds + k * kStageBytes<D>, n0 + i + k == 0);
+        if (i + k == ne) break;   // (the last fetch's last: values[0] is still the last stage's)
+        if (has_rows) compute_stage(i + k, lds + k * kKeyBytes<D>, values[n0 + i + k == 0 ? 1 : 0]);
         __syncthreads();
+        char* const free = values[0];
+        values[0] = values[1];
+        values[1] = values[2];
+        values[2] = free;
       }
     }
   }
+  if (has_rows && stages > 0) products_of(1, values[0], [](int) {});
+  __syncthreads();   // the LDS is the next segment's
 
 #pragma unroll
   for (int mt = 0; mt < R; ++mt) {
     const int r = row0 + mt * 16 + l16;
+    const float l = over_lane_groups_sum(l_run[mt]);
     if (r >= M) continue;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) store_state<D>(sh, in, part, out, seg, r, nt * 16 + qd * 4, o[mt][nt], m_run[mt], l_sum[mt][0]);
+    for (int nt = 0; nt < NT; ++nt) store_state<D>(sh, in, part, out, seg, r, nt * 16 + qd * 4, o[mt][nt], m_run[mt], l);
   }
 }
 
@@ -891,7 +948,7 @@ template <int D, int GP, int R>
 __global__ __launch_bounds__(512) void packed_rows_kernel(LOSA_PACKED_ARGS) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   constexpr int kRows = 128 * R;
-  int* plan = reinterpret_cast<int*>(lds) + 2 * kStageBytes<D> / 4;
+  int* plan = reinterpret_cast<int*>(lds) + kStagedBytes<D> / 4;
   for_each_segment<GP, kRows, 4>(kv, sh, in, part, out, heads, workgroups, least_tiles, plan, [&](const Segment& s) {
     for (int row0 = 0; row0 < s.M; row0 += kRows) packed_rows_body<D, GP, R>(kv, sh, in, pk, s, row0, part, out, scale_log2e, reinterpret_cast<char*>(lds));
   });
@@ -1033,7 +1090,7 @@ static hipError_t launch_dg(hipStream_t st, int dtype, const KvView& kv, const S
   if (rows <= 32) return go(packed_attn_kernel<D, GP, 2, 1>, DealtLds<2, D, 1>::kBytes, set[5]);
   if (rows <= 48) return go(packed_attn_kernel<D, GP, 3, 1>, DealtLds<3, D, 1>::kBytes, set[6]);
   if (rows <= 64) return go(packed_attn_kernel<D, GP, 2, 1, 2>, DealtLds<2, D, 1, 2>::kBytes, set[7]);
-  return rows <= 128 ? go(packed_rows_kernel<D, GP, 1>, 2 * kStageBytes<D>, set[8], 8) : go(packed_rows_kernel<D, GP, 2>, 2 * kStageBytes<D>, set[9], 8);
+  return rows <= 128 ? go(packed_rows_kernel<D, GP, 1>, kStagedBytes<D>, set[8], 8) : go(packed_rows_kernel<D, GP, 2>, kStagedBytes<D>, set[9], 8);
 }
 
 hipError_t launch_packed_attn(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, const AttnInputs& in, const PackedView& pk, int workgroups,
