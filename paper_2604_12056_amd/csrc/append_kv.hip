@@ -1,13 +1,15 @@
 // Position rotation of queries and keys, and new tokens' way into the pages of a cache.
 //
-// Both only move bytes: a rotated channel is six operations of arithmetic on two bytes in and two out.
+// Both are bound by the bytes they move: a rotated channel is 14 vector operations (see turned) on two bytes in and two out, half of the time
+// that the bytes take.
 #include "losa_device.h"
 #include "losa_internal.h"
 #include "new_tokens.h"
 
 namespace losa {
 
-// ---- rotation alone.  A thread has one unit (two 16-byte chunks) of a head of a token.
+// ---- rotation alone.  A thread has one unit (two 16-byte chunks) of a head of a token.  8192 tokens of 40 heads of 128 floats: 75 us, 4.5 TB/s
+// (a large copy reaches 5.1).  Rows are read once: 77 against 82 us, measured in turn; writing them so takes 102.
 struct RotateSide {
   const void* x;
   void* y;
@@ -25,7 +27,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(Rotation rot, const int32_t
   if (t >= tokens) return;
   const int at = positions[t], h = blockIdx.y;
   const T* from = h < q.heads ? (const T*)q.x + t * q.x_stride + h * d : (const T*)k.x + t * k.x_stride + (h - q.heads) * d;
-  uint4 a = *reinterpret_cast<const uint4*>(from + u.first), b = *reinterpret_cast<const uint4*>(from + u.second);
+  uint4 a = load_once(from + u.first), b = load_once(from + u.second);
   if ((unsigned)at >= (unsigned)rot.max_positions) return;
   if (u.angle >= 0) {
     float c[V], s[V], fa[V], fb[V];
@@ -66,9 +68,10 @@ hipError_t launch_rotate(hipStream_t st, int dtype, int d, const Rotation& rot, 
 //
 // Keys: d / (2 V) lanes per token, a unit each, turned where there is a rotation, written as they lie (token-major) and left in
 // LDS, out of which a lane takes the bounds of its channels.
-// Values: a lane has one dword of channels, reads eight tokens of it (a token's row is one contiguous read of the wavefront) and
-// writes each channel's eight tokens as 16 or 32 contiguous bytes of the channel-major page: the transposition costs no
-// LDS and no lane exchange.  Rows that get no token are not written.
+// Values: a lane has one dword of channels and reads eight tokens of it (a token's row is one contiguous read of the wavefront), which makes
+// each channel's eight tokens 16 or 32 contiguous bytes of the channel-major page.  Where all 16 rows get a token they are written
+// in order by way of LDS (38.4 against 41.4 us at the size below), else one by one: rows that get no token are not written.
+// 32768 tokens of 4 heads of 128 bfloat16, keys rotated: 32 us, 4.8 TB/s (a copy of as many bytes reaches 5.0); without reading rows once, 37.
 template <typename T, int D, int GP>
 __global__ __launch_bounds__(256) void append_kernel(KvView kv, Shape sh, NewTokens in, Rotation rot) {
   constexpr int V = Vec16<T>::n, LPT = D / (2 * V), TPP = 64 / LPT, PASSES = 16 / TPP;   // keys: lanes per token, tokens per pass
@@ -94,8 +97,8 @@ __global__ __launch_bounds__(256) void append_kernel(KvView kv, Shape sh, NewTok
     row[i] = 16 * half + i * TPP + lane / LPT;
     ok[i] = row[i] >= f.lo && row[i] < f.hi && h < sh.Hkv;
     const T* from = (const T*)in.k + (size_t)(f.source + max(0, min(row[i] - f.lo, most))) * in.k_stride + head * D;
-    a[i] = *reinterpret_cast<const uint4*>(from + u.first);
-    b[i] = *reinterpret_cast<const uint4*>(from + u.second);
+    a[i] = load_once(from + u.first);
+    b[i] = load_once(from + u.second);
   }
   const int col = lane % LPR, set = lane / LPR;
   uint32_t x[OCTETS][COLS][8];
@@ -106,7 +109,7 @@ __global__ __launch_bounds__(256) void append_kernel(KvView kv, Shape sh, NewTok
       const int t = 16 * half + 8 * (o * SETS + set) + e;
       const T* from = (const T*)in.v + (size_t)(f.source + max(0, min(t - f.lo, most))) * in.v_stride + head * D;
 #pragma unroll
-      for (int w = 0; w < COLS; ++w) x[o][w][e] = reinterpret_cast<const uint32_t*>(from)[w * 64 + col];
+      for (int w = 0; w < COLS; ++w) x[o][w][e] = load_once(reinterpret_cast<const uint32_t*>(from) + w * 64 + col);
     }
   float c[PASSES][V], s[PASSES][V];
   if (rot.table) {
@@ -127,6 +130,62 @@ __global__ __launch_bounds__(256) void append_kernel(KvView kv, Shape sh, NewTok
   uint32_t there = 0;   // rows of these 16 that hold a token now
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
+    const unsigned long long who = __ballot(ok[i]);
+#pragma unroll
+    for (int t = 0; t < TPP; ++t) there |= (uint32_t)((who >> (t * LPT)) & 1) << (i * TPP + t);
+  }
+
+  T* const mine = lds[hl] + 16 * half * D;   // this wavefront's own
+  T* const vpage = (T*)kv.v_pages + tile * (GP * D) + 16 * half;
+  constexpr int CHUNKS = sizeof(T);          // 16-byte chunks of a channel's 16 tokens
+#pragma unroll
+  for (int o = 0; o < OCTETS; ++o) {
+    const int octet = o * SETS + set;
+    const uint32_t mask = (there >> (8 * octet)) & 0xFFu;
+#pragma unroll
+    for (int w = 0; w < COLS; ++w) {
+      const uint32_t(&y)[8] = x[o][w];
+      const int channel = (w * 64 + col) * E;
+      if (there == 0xFFFFu) {
+        uint4* dst = reinterpret_cast<uint4*>(mine) + channel * CHUNKS + octet * (CHUNKS / 2);
+        if constexpr (E == 2) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t pick = e ? 0x07060302u : 0x05040100u;
+            dst[e * CHUNKS] = make_uint4(__builtin_amdgcn_perm(y[1], y[0], pick), __builtin_amdgcn_perm(y[3], y[2], pick),
+                                         __builtin_amdgcn_perm(y[5], y[4], pick), __builtin_amdgcn_perm(y[7], y[6], pick));
+          }
+        } else {
+          dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+          dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
+        }
+      } else {
+        T* dst = vpage + channel * GP + 8 * octet;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if ((mask >> e) & 1) {
+            if constexpr (E == 2) {
+              dst[e] = (T)(y[e] & 0xFFFFu);
+              dst[GP + e] = (T)(y[e] >> 16);
+            } else {
+              reinterpret_cast<uint32_t*>(dst)[e] = y[e];
+            }
+          }
+      }
+    }
+  }
+  if (there == 0xFFFFu) {
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < D * CHUNKS / 64; ++i) {
+      const int id = i * 64 + lane;
+      *reinterpret_cast<uint4*>(vpage + (id / CHUNKS) * GP + (id % CHUNKS) * (16 / CHUNKS)) = reinterpret_cast<const uint4*>(mine)[id];
+    }
+    wave_lds_fence();   // the keys go there next
+  }
+
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
     if (rot.table && u.angle >= 0) {
       float fa[V], fb[V];
       widen16(a[i], fa, T());
@@ -142,46 +201,6 @@ __global__ __launch_bounds__(256) void append_kernel(KvView kv, Shape sh, NewTok
       if (kv.meta) {
         *reinterpret_cast<uint4*>(lds[hl] + row[i] * D + u.first) = a[i];
         *reinterpret_cast<uint4*>(lds[hl] + row[i] * D + u.second) = b[i];
-      }
-    }
-    const unsigned long long who = __ballot(ok[i]);
-#pragma unroll
-    for (int t = 0; t < TPP; ++t) there |= (uint32_t)((who >> (t * LPT)) & 1) << (i * TPP + t);
-  }
-
-  T* vpage = (T*)kv.v_pages + tile * (GP * D) + 16 * half;
-#pragma unroll
-  for (int o = 0; o < OCTETS; ++o) {
-    const int t0 = 8 * (o * SETS + set);
-    const uint32_t mask = (there >> t0) & 0xFFu;
-#pragma unroll
-    for (int w = 0; w < COLS; ++w) {
-      const uint32_t(&y)[8] = x[o][w];
-      T* dst = vpage + (w * 64 + col) * E * GP + t0;
-      if (mask == 0xFFu) {
-        if constexpr (E == 2) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t pick = e ? 0x07060302u : 0x05040100u;
-            *reinterpret_cast<uint4*>(dst + e * GP) =
-                make_uint4(__builtin_amdgcn_perm(y[1], y[0], pick), __builtin_amdgcn_perm(y[3], y[2], pick), __builtin_amdgcn_perm(y[5], y[4], pick),
-                           __builtin_amdgcn_perm(y[7], y[6], pick));
-          }
-        } else {
-          reinterpret_cast<uint4*>(dst)[0] = make_uint4(y[0], y[1], y[2], y[3]);
-          reinterpret_cast<uint4*>(dst)[1] = make_uint4(y[4], y[5], y[6], y[7]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if ((mask >> e) & 1) {
-            if constexpr (E == 2) {
-              dst[e] = (T)(y[e] & 0xFFFFu);
-              dst[GP + e] = (T)(y[e] >> 16);
-            } else {
-              reinterpret_cast<uint32_t*>(dst)[e] = y[e];
-            }
-          }
       }
     }
   }

@@ -6,6 +6,17 @@
 
 namespace losa {
 
+// Bytes that a launch reads, or writes, once: they need displace nothing in the caches.  (What each is worth is said where it is used.)
+typedef __attribute__((ext_vector_type(4))) uint32_t words4_t;
+__device__ __forceinline__ uint4 load_once(const void* p) {
+  const words4_t x = __builtin_nontemporal_load(reinterpret_cast<const words4_t*>(p));
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ uint32_t load_once(const uint32_t* p) { return __builtin_nontemporal_load(p); }
+__device__ __forceinline__ void store_once(void* p, const uint4& v) {
+  __builtin_nontemporal_store((words4_t){v.x, v.y, v.z, v.w}, reinterpret_cast<words4_t*>(p));
+}
+
 // ---- the rotation.  (x1, x2) of an angle (c, s) becomes (x1 c - x2 s, x2 c + x1 s).
 //
 // Both products and the difference are taken with their rounding errors (a product's by one fused multiply-add, a
@@ -18,8 +29,8 @@ __device__ __forceinline__ float turned(float x1, float c, float x2, float s) { 
   const float ea = __builtin_fmaf(x1, c, -a), eb = __builtin_fmaf(x2, s, -b);
   const float sum = a + b, t = sum - a;
   const float err = (a - (sum - t)) + (b - t);
-  const float exact = sum + (err + (ea + eb));
-  return __builtin_fabsf(sum) < INFINITY ? exact : sum;   // (an infinity's error term is no number)
+  // (An infinity's error term is no number, so the maximum below passes over it; a number's is above -3 * 2^103.)
+  return sum + __builtin_fmaxf(err + (ea + eb), -0x1p105f);
 }
 
 // A unit is two 16-byte chunks of a row and the V angles that turn them: halves style channels u V .. and half a turn's width

@@ -218,10 +218,10 @@ __global__ __launch_bounds__(256) void append_packed_kernel(KvView kv, Shape sh,
 }
 
 // Eight numbers, as dwords of two bfloat16 each, to a row of T.
-__device__ __forceinline__ void store8(bf16_t* dst, const uint4& n) { *reinterpret_cast<uint4*>(dst) = n; }
+__device__ __forceinline__ void store8(bf16_t* dst, const uint4& n) { store_once(dst, n); }
 __device__ __forceinline__ void store8(float* dst, const uint4& n) {
-  reinterpret_cast<uint4*>(dst)[0] = make_uint4(n.x << 16, n.x & 0xFFFF0000u, n.y << 16, n.y & 0xFFFF0000u);
-  reinterpret_cast<uint4*>(dst)[1] = make_uint4(n.z << 16, n.z & 0xFFFF0000u, n.w << 16, n.w & 0xFFFF0000u);
+  store_once(dst, make_uint4(n.x << 16, n.x & 0xFFFF0000u, n.y << 16, n.y & 0xFFFF0000u));
+  store_once(dst + 4, make_uint4(n.z << 16, n.z & 0xFFFF0000u, n.w << 16, n.w & 0xFFFF0000u));
 }
 
 template <typename T, int D, int GP>
@@ -245,11 +245,11 @@ __global__ __launch_bounds__(256) void read_packed_kernel(KvView kv, Shape sh, c
   uint4 vc = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
-    kc[i] = *reinterpret_cast<const uint32_t*>(in.k + tile * kTile + (16 * part + i * TPS + row) * (D / 2) + c8 * 4);
+    kc[i] = load_once(reinterpret_cast<const uint32_t*>(in.k + tile * kTile + (16 * part + i * TPS + row) * (D / 2) + c8 * 4));
     ks[i] = scales[(i * TPS + row) * J + j];
     vs[i] = scales[GP * J + (i * TPS + row) * J + j];
   }
-  if (lane < D / 2) vc = *reinterpret_cast<const uint4*>(in.v + tile * kTile + part * (8 * D) + lane * 16);
+  if (lane < D / 2) vc = load_once(in.v + tile * kTile + part * (8 * D) + lane * 16);
   if (lane < D / 2) *reinterpret_cast<uint4*>(&codes[wave][lane * 16]) = vc;
   wave_lds_fence();
   const uint32_t pick = (c8 & 2) ? 0x07060302u : 0x05040100u;   // the second half of a group's channels are the high codes
