@@ -533,7 +533,9 @@ losa_status packed_attn_impl(losa_ctx* ctx, hipStream_t st, const KvView& kv, co
     part.l = part.m + room * part.rows;
   }
   const long target = ctx->target_workgroups * (known && rows_upper > kSparseRows && ctx->cfg.dtype == LOSA_BF16 ? 1 : 2);
-  const long workgroups = heads <= kPlannedHeads && room - heads >= kTargetWorkgroups / 2 ? std::min(target, room - heads) : 0;
+  // (The shares are counted in 32 bits: a row tile of 16 costs three units a tile of 32 tokens at most, and a list's start and end 16 tiles.)
+  const bool countable = heads * ((long)ctx->sh.max_pages * ctx->sh.g / 32 + 17) * ((rows_upper + 15) / 16 * 3) < (1L << 30);
+  const long workgroups = heads <= kPlannedHeads && countable && room - heads >= kTargetWorkgroups / 2 ? std::min(target, room - heads) : 0;
   const AttnInputs in{q, active_idx, active_count, sel_pages, sel_count, cap};
   const PackedOut out{o_p, lse_p, (int2*)ctx->union_bits};
   hipError_t e;
