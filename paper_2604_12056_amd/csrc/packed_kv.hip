@@ -4,6 +4,11 @@
 // Packing: a lane has one token's group of 32 channels, what a scale is made of, and the 16 bytes that come of it; a wavefront has
 // 16 tokens of a page and head (32 with 64 channels in a page of 32).  Reading: a lane has eight channels of a token, 16 bytes of what is
 // written.  A workgroup is four wavefronts of a page: two halves of two heads, or four heads.
+//
+// Packing 4 x 4093 tokens (and fewer) of 8 heads of 128, pages of 32, keys turned: 29 us for 88 MB; what the bytes leave is the turning and the
+// latency of three wavefronts a SIMD (angles for 32 channels take 64 registers).  Values a byte at a time: 37 us.  Rows read past the caches: 34, as
+// a lane's 64 bytes are four requests of one line.  Single tokens of 16 sequences: 6 us, four dependent trips to memory.
+// Reading two sequences of 39012 tokens in all: 26.5 us, 5.3 TB/s (codes and rows past the caches: 29.1 without).
 #include "losa_device.h"
 #include "losa_internal.h"
 #include "new_tokens.h"
