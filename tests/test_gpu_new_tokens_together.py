@@ -90,6 +90,20 @@ def test_rows_beyond_32_bit_offsets():
     ctx.close()
 
 
+def test_many_tokens_are_turned_as_few_are():
+    n = 9001
+    ctx, rot, pos = context(3, 1, 4, 1, 1), table(512), torch.arange(n, dtype=torch.int32, device=DEV) % 512
+    q, k = rows(6, n, 3, D), rows(7, n, 1, D)
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    L.losa_rotate(ctx, rot, pos, q, qo, k, ko)
+    for a in range(0, n, 1000):
+        at = slice(a, min(a + 1000, n))
+        qs, ks = torch.zeros_like(q[at]), torch.zeros_like(k[at])
+        L.losa_rotate(ctx, rot, pos[at], q[at], qs, k[at], ks)
+        assert torch.equal(qo[at], qs) and torch.equal(ko[at], ks)
+    ctx.close()
+
+
 class Cache:
     """A 4-bit cache, its context and what goes through them."""
 
