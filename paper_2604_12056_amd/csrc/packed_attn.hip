@@ -412,8 +412,8 @@ __device__ __forceinline__ void packed_attn_body(const KvView& kv, const Shape& 
       const uint32_t key = l16 * 64 + qd * 16, value = lane * 16, second = GP == 16 ? 0 : 1024;
       start_to_lds(pk.k + t0 * kPageBytes, key, to);
       start_to_lds(pk.k + t1 * kPageBytes + second, key, to + 1024);
-      start_to_lds(pk.v + t0 * kPageBytes, value, to + 2048);
-      start_to_lds(pk.v + t1 * kPageBytes + second, value, to + 3072);
+      start_to_lds(pk.v + t0 * kPageBytes, value, to + 2 * 1024);
+      start_to_lds(pk.v + t1 * kPageBytes + second, value, to + 3 * 1024);
     } else {
       // two pages' 512 bytes are a load: lanes 32 .. 63 have the second's
       const size_t from = GP == 16 ? (lane < 32 ? t0 : t1) * kPageBytes + (lane & 31) * 16 : t0 * kPageBytes + lane * 16;
