@@ -198,3 +198,46 @@ def test_recorded_and_eager_calls_in_turn():
         assert all(torch.equal(x, y) for x, y in zip(want[i], c.state())), i
     c.ctx.close()
     other.ctx.close()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_stages_one_by_one_over_a_packed_cache(shared):
+    """Active set, pages by the packed keys' bounds, attention: call by call what losa_step_packed does in one (or with one list per head).
+
+    Tolerance: both results are within 4 ds + (n + 70) u of the exact ones, in units of the largest value, and lse within ds + (n + 70) u + 4 u |lse|
+    (u = 2^-24, ds = (d + 4) u S + 4 u; derived in test_gpu_packed_attn.py).  n <= 224 tokens; S <= 2 |q| |k| / sqrt(d) + 16 <= 80, as rows of 128 normal
+    numbers are shorter than 16 and rounding to 4 bits adds a third at most; |lse| < 32."""
+    c = Cache(50)
+    c.fill()
+    B, batch, Hkv, most = c.B, 3, 2, 3
+    h_prev, step = rows(51, batch * B, c.ctx.q_heads * D), rows(52, batch * B, c.ctx.q_heads * D)
+    h_cur = h_prev + step * (torch.arange(batch * B, device=DEV) % 3 == 0)[:, None]
+    assert c.q.float().norm(dim=2).max() < 16 and torch.cat((c.prompt[0], c.k)).float().norm(dim=2).max() < 16
+    o, lse = torch.zeros_like(c.o), torch.zeros_like(c.lse)
+    mask, count = torch.zeros(batch * B, dtype=torch.uint8, device=DEV), torch.zeros((batch, Hkv), dtype=torch.int32, device=DEV)
+    L.losa_step_packed(c.ctx, c.kv, 1, h_cur, h_prev, c.q, L.LOSA_SEL_TOPK, 3.0, most, o, lse, mask, count)
+    torch.cuda.synchronize()
+    cap = max((n + 3 * B + G - 1) // G for n in c.lens0)
+    delta, mask2 = torch.zeros(batch * B, device=DEV), torch.zeros_like(mask)
+    idx, n = torch.full((batch, B), -1, dtype=torch.int32, device=DEV), torch.zeros(batch, dtype=torch.int32, device=DEV)
+    L.losa_select_active(c.ctx, h_cur, h_prev, L.LOSA_SEL_TOPK, 3.0, delta, mask2, idx, n)
+    pages, count2 = torch.full((batch, Hkv, cap), -1, dtype=torch.int32, device=DEV), torch.zeros_like(count)
+    if shared:
+        L.losa_score_pages_shared(c.ctx, c.kv.for_scoring(), c.q, idx, n, most, pages, count2, cap)
+    else:
+        L.losa_score_pages(c.ctx, c.kv.for_scoring(), c.q, idx, n, most, None, pages, count2, cap)
+    L.losa_sparse_attn_packed(c.ctx, c.kv, c.q, idx, n, pages, count2, cap, c.o, c.lse)
+    torch.cuda.synchronize()
+    assert torch.equal(mask, mask2) and int(mask.sum()) == 3 * batch
+    held = [(x + G - 1) // G for x in c.lens0]
+    if shared:
+        assert count2.tolist() == [[min(most, m)] * Hkv for m in held]
+        assert bool(c.lse[mask.bool()].isfinite().all())
+        return c.ctx.close()
+    assert torch.equal(count, count2)
+    biggest = torch.cat((c.prompt[1], c.v)).float().abs().max() * 4 / 3
+    u, ds = 2.0 ** -24, (132 * 80 + 4) * 2.0 ** -24
+    assert float((o - c.o).abs().max()) <= 2 * (4 * ds + 294 * u) * float(biggest)
+    assert float((lse - c.lse)[mask.bool()].abs().max()) <= 2 * (ds + 294 * u + 4 * u * 32)
+    assert not o[~mask.bool()].any() and not c.o[~mask.bool()].any()
+    c.ctx.close()
