@@ -266,6 +266,22 @@ __device__ __forceinline__ void for_each_segment(const KvView& kv, const Shape& 
   }
 }
 
+// The block token of row r of a sequence, and the output row that is (negative: none).
+__device__ __forceinline__ int token_of(const Shape& sh, const AttnInputs& in, int b, int r) {
+  const int a = row_token(sh, r);
+  return in.active_idx ? in.active_idx[(size_t)b * sh.B + a] : a;
+}
+__device__ __forceinline__ long output_row(const Shape& sh, int b, int j, int r, int tok) {
+  return (unsigned)tok < (unsigned)sh.B ? ((long)b * sh.B + tok) * sh.Hq + j * sh.G + (r - row_token(sh, r) * sh.G) : -1;
+}
+template <int D>
+__device__ __forceinline__ void store_output(const PackedOut& out, long row, int channel, f32x4_t acc, float m, float l) {
+  if (row < 0) return;
+  const bool any = m > -1.0e29f || l != l;   // no valid token at all: the neutral element of a merge.  (Scores that are all NaN move no reference)
+  *reinterpret_cast<f32x4_t*>(out.o_p + row * D + channel) = any ? acc / l : (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  if (channel == 0) out.lse_p[row] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
 // A vector of four channels of row r of a segment, numerators against `m` with sum `l`: a partial's, or the finished output.
 template <int D>
 __device__ __forceinline__ void store_state(const Shape& sh, const AttnInputs& in, const Partials& part, const PackedOut& out, const Segment& s, int r, int channel,
@@ -279,12 +295,7 @@ __device__ __forceinline__ void store_state(const Shape& sh, const AttnInputs& i
     *reinterpret_cast<f32x4_t*>(part.o + (size_t)prow * D + channel) = acc;
     return;
   }
-  const int a = row_token(sh, r), tok = in.active_idx ? in.active_idx[(size_t)s.b * sh.B + a] : a;
-  if ((unsigned)tok >= (unsigned)sh.B) return;
-  const size_t orow = ((size_t)s.b * sh.B + tok) * sh.Hq + s.j * sh.G + (r - a * sh.G);
-  const bool any = m > -1.0e29f || l != l;   // no valid token at all: the neutral element of a merge.  (Scores that are all NaN move no reference)
-  *reinterpret_cast<f32x4_t*>(out.o_p + orow * D + channel) = any ? acc / l : (f32x4_t){0.f, 0.f, 0.f, 0.f};
-  if (channel == 0) out.lse_p[orow] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  store_output<D>(out, output_row(sh, s.b, s.j, r, token_of(sh, in, s.b, r)), channel, acc, m, l);
 }
 
 // Sixteen bytes a lane from `base` + offset to LDS at `to` + 16 lane, without a register on the way.  The wavefront waits for them itself (landed()).
@@ -991,16 +1002,15 @@ __global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, A
   __shared__ __attribute__((aligned(16))) float4 red[CL][C4];
   __shared__ float2 stats[CL];
   const int tid = threadIdx.x, cl = tid / C4, c4 = tid % C4, head = blockIdx.y, b = head / sh.Hkv;
+  const int j = head - b * sh.Hkv;
+  // asked for with the counts: the token of a thread's first row, of which it has one only as a rule
+  const int first_r = min((int)blockIdx.x * CL + cl, sh.rows_max - 1), first_tok = token_of(sh, in, b, first_r);
   int n = __builtin_amdgcn_readfirstlane((in.active_count ? in.active_count : kv.seq_lens)[b]);
   int first = __builtin_amdgcn_readfirstlane(out.table[head].x), items = __builtin_amdgcn_readfirstlane(out.table[head].y);
-  asm("" : "+s"(n), "+s"(first), "+s"(items) : "s"(sh.B), "s"(sh.G));   // (one memory round trip; see Sequence)
+  asm("" : "+s"(n), "+s"(first), "+s"(items) : "s"(sh.B), "s"(sh.G), "s"(sh.rows_max), "s"(part.rows), "s"(part.m), "s"(part.l), "s"(part.o));   // (one round trip; see Sequence)
   if (items == 1) return;   // finished already
   const int M = min((in.active_count ? min(n, sh.B) : sh.B) * sh.G, min(sh.rows_max, part.rows));
   const bool few = items <= kFewItems;
-  Segment s;
-  s.b = b;
-  s.j = head - b * sh.Hkv;
-  s.item = -1;
   // items lane, lane + step, ... of row r
   auto gather = [&](int r, int lane, int step, float& m, float& l, f32x4_t& acc) {
     m = kNegBig;
@@ -1039,7 +1049,8 @@ __global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, A
       float m, l;
       f32x4_t acc;
       gather(r, 0, 1, m, l, acc);
-      store_state<D>(sh, in, part, out, s, r, c4 * 4, acc, m, l);
+      const int tok = r == first_r ? first_tok : token_of(sh, in, b, r);
+      store_output<D>(out, output_row(sh, b, j, r, tok), c4 * 4, acc, m, l);
     }
     return;
   }
@@ -1062,7 +1073,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(KvView kv, Shape sh, A
         l_all = fmaf(stats[k].y, wgt, l_all);
         o += (f32x4_t){x.x, x.y, x.z, x.w} * wgt;
       }
-      store_state<D>(sh, in, part, out, s, r, c4 * 4, o, m_all, l_all);
+      store_output<D>(out, output_row(sh, b, j, r, token_of(sh, in, b, r)), c4 * 4, o, m_all, l_all);
     }
     __syncthreads();   // the LDS is the next row's
   }
