@@ -29,14 +29,6 @@ __device__ __forceinline__ int scale_byte(float top, int least, int most) {
 }
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// The largest magnitude of 32 numbers, NaN if one of them is: in the bits of magnitudes, integers order as the numbers do and NaN is largest.
-__device__ __forceinline__ float largest(const float (&x)[32]) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int e = 0; e < 32; ++e) m = max(m, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-  return __uint_as_float(m);
-}
-
 // Two numbers' codes in byte SEL of a dword, `a` in its low four bits; to nearest, ties to even, saturating at 6.
 template <int SEL>
 __device__ __forceinline__ uint32_t put_codes(uint32_t old, float a, float b, float scale) {

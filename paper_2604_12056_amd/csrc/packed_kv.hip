@@ -16,23 +16,26 @@
 
 namespace losa {
 
-// 32 channels of a row as they lie, and widened.
+// A lane's share of a group of 32 channels: eight of its first half and the same eight of its second, 16 further (c: the first).
+// Neighbouring lanes have the two shares of a group.
+constexpr int kShare = 16;
 template <typename T>
-struct Raw32 {
-  uint4 v[32 / Vec16<T>::n];
+struct RawShare {
+  uint4 v[kShare / Vec16<T>::n];
 };
 template <typename T>
-__device__ __forceinline__ Raw32<T> load32(const T* p) {
-  Raw32<T> r;
+__device__ __forceinline__ RawShare<T> load_share(const T* p) {
+  constexpr int V = Vec16<T>::n;
+  RawShare<T> r;
 #pragma unroll
-  for (int i = 0; i < 32 / Vec16<T>::n; ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+  for (int i = 0; i < kShare / V; ++i) r.v[i] = *reinterpret_cast<const uint4*>(p + 16 * (i * V / 8) + i * V % 8);
   return r;
 }
 template <typename T>
-__device__ __forceinline__ void widen32(const Raw32<T>& r, float (&x)[32]) {
+__device__ __forceinline__ void widen_share(const RawShare<T>& r, float (&x)[kShare]) {
   constexpr int V = Vec16<T>::n;
 #pragma unroll
-  for (int i = 0; i < 32 / V; ++i) {
+  for (int i = 0; i < kShare / V; ++i) {
     float f[V];
     widen16(r.v[i], f, T());
 #pragma unroll
@@ -40,21 +43,21 @@ __device__ __forceinline__ void widen32(const Raw32<T>& r, float (&x)[32]) {
   }
 }
 
-// What turns channels c .. c + 31 of a row: their angles and, halves style, the channels half a turn's width away.  Eight channels are turned by a whole
+// What turns a share: its angles and, halves style, the channels half a turn's width away.  Eight channels are turned by a whole
 // half or not at all, as rotary_dim is a multiple of 16.  (No branch around a load: what does not turn, or has its pair at hand, loads something and
 // does not use it.)
 template <typename T>
-struct Turn32 {
-  float4 cs[8], sn[8];   // pairs style: every other one counts
-  uint4 other[32 / Vec16<T>::n];
+struct TurnShare {
+  float4 cs[4], sn[4];   // pairs style: every other one counts
+  uint4 other[kShare / Vec16<T>::n];
 };
 template <typename T>
-__device__ __forceinline__ void load_turn32(const T* row, int c, const float* angles, const Rotation& rot, Turn32<T>& t) {
+__device__ __forceinline__ void load_turn(const T* row, int c, const float* angles, const Rotation& rot, TurnShare<T>& t) {
   constexpr int V = Vec16<T>::n;
   const int half = rot.rotary / 2, next = rot.pairs ? 0 : 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int ch = c + 8 * i, in = ch < rot.rotary ? ch : 0;
+  for (int i = 0; i < 2; ++i) {
+    const int ch = c + 16 * i, in = ch < rot.rotary ? ch : 0;
     const int at = rot.pairs ? in / 2 : in < half ? in : in - half;
     const int away = rot.pairs || ch >= rot.rotary ? ch : ch < half ? ch + half : ch - half;
 #pragma unroll
@@ -68,12 +71,12 @@ __device__ __forceinline__ void load_turn32(const T* row, int c, const float* an
 }
 // x, turned and rounded to T, as a cache of T would hold it.
 template <typename T>
-__device__ __forceinline__ void turn32(float (&x)[32], int c, const Rotation& rot, const Turn32<T>& t) {
+__device__ __forceinline__ void turn_share(float (&x)[kShare], int c, const Rotation& rot, const TurnShare<T>& t) {
   constexpr int V = Vec16<T>::n;
   const int half = rot.rotary / 2;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int ch = c + 8 * i;
+  for (int i = 0; i < 2; ++i) {
+    const int ch = c + 16 * i;
     float y[8];
     if (rot.pairs) {
       const float4 c0 = t.cs[2 * i], s0 = t.sn[2 * i];
@@ -109,74 +112,77 @@ __device__ __forceinline__ void turn32(float (&x)[32], int c, const Rotation& ro
   }
 }
 
-// Codes of 32 numbers: byte i of the result holds x[FIRST i] and x[FIRST i + SECOND] (keys: neighbours; values: 16 apart).
-template <int FIRST, int SECOND>
-__device__ __forceinline__ uint4 codes_of(const float (&x)[32], int byte) {
-  const float scale = power_of(byte);
-  uint32_t w[4];
+// The largest magnitude of a group, both lanes' shares, NaN if one of its numbers is: in the bits of magnitudes, integers order as the numbers do and NaN is
+// largest.
+__device__ __forceinline__ float largest(const float (&x)[kShare]) {
+  uint32_t m = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint32_t c = 0;
-    c = put_codes<0>(c, x[FIRST * (4 * k)], x[FIRST * (4 * k) + SECOND], scale);
-    c = put_codes<1>(c, x[FIRST * (4 * k + 1)], x[FIRST * (4 * k + 1) + SECOND], scale);
-    c = put_codes<2>(c, x[FIRST * (4 * k + 2)], x[FIRST * (4 * k + 2) + SECOND], scale);
-    c = put_codes<3>(c, x[FIRST * (4 * k + 3)], x[FIRST * (4 * k + 3) + SECOND], scale);
-    w[k] = byte == kScaleNaN ? 0u : c;
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int e = 0; e < kShare; ++e) m = max(m, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+  return __uint_as_float(max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, true)));   // (lanes 1 0 3 2 of every four)
+}
+
+// A dword of codes: byte i holds a[FIRST i] and b[FIRST i].
+template <int FIRST>
+__device__ __forceinline__ uint32_t four_codes(const float* a, const float* b, int byte) {
+  const float scale = power_of(byte);
+  uint32_t c = 0;
+  c = put_codes<0>(c, a[0], b[0], scale);
+  c = put_codes<1>(c, a[FIRST], b[FIRST], scale);
+  c = put_codes<2>(c, a[2 * FIRST], b[2 * FIRST], scale);
+  c = put_codes<3>(c, a[3 * FIRST], b[3 * FIRST], scale);
+  return byte == kScaleNaN ? 0u : c;
 }
 
 template <int D, int GP>
 struct PageWork {   // of a workgroup
-  static constexpr int J = D / 32, TPP = 64 / J < GP ? 64 / J : GP;   // groups per token, tokens per wavefront
-  static constexpr int PASSES = GP / TPP, HEADS = 4 / PASSES;         // wavefronts per page and head, heads per workgroup
+  static constexpr int LPT = D / kShare, TPP = 64 / LPT;        // lanes per token, tokens per wavefront
+  static constexpr int PASSES = GP / TPP, HEADS = 4 / PASSES;   // wavefronts per page and head, heads per workgroup
 };
 
 template <typename T, int D, int GP>
 __global__ __launch_bounds__(256) void append_packed_kernel(KvView kv, Shape sh, NewTokens in, Rotation rot, PackedView out) {
   typedef PageWork<D, GP> Work;
-  constexpr int J = Work::J, TPP = Work::TPP, kTile = GP * D / 2;
+  constexpr int J = D / 32, LPT = Work::LPT, TPP = Work::TPP, kTile = GP * D / 2, kWaveBytes = TPP * D / 2;
   __shared__ __attribute__((aligned(16))) T keys[Work::HEADS][GP * D];   // the numbers that stand for the keys, for the page's bounds
-  __shared__ __attribute__((aligned(16))) uint8_t codes[4][TPP * D / 2];
+  __shared__ __attribute__((aligned(16))) uint8_t codes[4][kWaveBytes];
   __shared__ uint32_t arrived[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int pass = wave % Work::PASSES, hl = wave / Work::PASSES, h = blockIdx.z * Work::HEADS + hl, j = lane % J;
+  const int pass = wave % Work::PASSES, hl = wave / Work::PASSES, h = blockIdx.z * Work::HEADS + hl;
+  const int j = lane % LPT / 2, part = lane & 1, c = 32 * j + 8 * part;   // group, which of its lanes, first channel
   const Fill f = fill_of(kv, sh, in.indptr, in.num_tokens, blockIdx.y, blockIdx.x);
   if (f.hi <= f.lo) return;
   const int phys = kv.page_indices[f.entry];
-  const int row = lane / J, t = pass * TPP + row;   // (with 64 channels and pages of 16 the upper lanes have no row)
-  const bool mine = row < TPP && t >= f.lo && t < f.hi && h < sh.Hkv;
+  const int row = lane / LPT, t = pass * TPP + row;
+  const bool mine = t >= f.lo && t < f.hi && h < sh.Hkv;
   const int at_row = max(f.lo, min(t, f.hi - 1)) - f.lo, src = f.source + at_row, head = min(h, sh.Hkv - 1);
   const T* const krow = (const T*)in.k + (size_t)src * in.k_stride + head * D;
-  const Raw32<T> kraw = load32<T>(krow + j * 32), vraw = load32<T>((const T*)in.v + (size_t)src * in.v_stride + head * D + j * 32);
+  const RawShare<T> kraw = load_share<T>(krow + c), vraw = load_share<T>((const T*)in.v + (size_t)src * in.v_stride + head * D + c);
   bool ok = mine;
-  Turn32<T> turn;
+  TurnShare<T> turn;
   if (rot.table) {
     const int at = in.positions ? in.positions[src] : f.slot + at_row;
     ok = mine && (unsigned)at < (unsigned)rot.max_positions;
-    load_turn32<T>(krow, j * 32, rot.table + (size_t)(ok ? at : 0) * rot.rotary, rot, turn);
+    load_turn<T>(krow, c, rot.table + (size_t)(ok ? at : 0) * rot.rotary, rot, turn);
   }
   if ((unsigned)phys >= (unsigned)kv.num_pages) return;
   const size_t tile = (size_t)phys * sh.Hkv + head;
   uint8_t* const scales = out.scales + tile * (2 * GP * J);
-  uint8_t* const vcodes = out.v + tile * kTile;
+  uint8_t* const vcodes = out.v + tile * kTile + pass * kWaveBytes;
 
-  float x[32];
-  widen32<T>(kraw, x);
-  if (rot.table) turn32<T>(x, j * 32, rot, turn);
+  float x[kShare];
+  widen_share<T>(kraw, x);
+  if (rot.table) turn_share<T>(x, c, rot, turn);
   const int byte = scale_byte(largest(x), kKeyScaleMin, kKeyScaleMax);
-  const uint4 c = codes_of<2, 1>(x, byte);
   if (ok) {
-    *reinterpret_cast<uint4*>(out.k + tile * kTile + t * (D / 2) + j * 16) = c;
-    scales[t * J + j] = (uint8_t)byte;
-    if (kv.meta) {
-      const float scale = power_of(byte);
-      const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    if (part == 0) scales[t * J + j] = (uint8_t)byte;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint4 n = make_uint4(codes_to_bf16<0>(w[k], scale), codes_to_bf16<1>(w[k], scale), codes_to_bf16<2>(w[k], scale),
-                                   codes_to_bf16<3>(w[k], scale));
-        uint4* dst = reinterpret_cast<uint4*>(&keys[hl][t * D + j * 32 + 8 * k]);
+    for (int i = 0; i < 2; ++i) {   // (neighbours are a byte)
+      const uint32_t w = four_codes<2>(x + 8 * i, x + 8 * i + 1, byte);
+      *reinterpret_cast<uint32_t*>(out.k + tile * kTile + t * (D / 2) + j * 16 + 8 * i + 4 * part) = w;
+      if (kv.meta) {
+        const float scale = power_of(byte);
+        const uint4 n = make_uint4(codes_to_bf16<0>(w, scale), codes_to_bf16<1>(w, scale), codes_to_bf16<2>(w, scale), codes_to_bf16<3>(w, scale));
+        uint4* dst = reinterpret_cast<uint4*>(&keys[hl][t * D + c + 16 * i]);
         if constexpr (sizeof(T) == 2) {
           dst[0] = n;
         } else {
@@ -186,38 +192,34 @@ __global__ __launch_bounds__(256) void append_packed_kernel(KvView kv, Shape sh,
       }
     }
   }
-  widen32<T>(vraw, x);
+  widen_share<T>(vraw, x);
   const int vbyte = scale_byte(largest(x), kValueScaleMin, kValueScaleMax);
-  const uint4 vc = codes_of<1, 16>(x, vbyte);
-  const uint32_t vw[4] = {vc.x, vc.y, vc.z, vc.w};
-  if (ok) scales[GP * J + t * J + j] = (uint8_t)vbyte;
+  if (ok && part == 0) scales[GP * J + t * J + j] = (uint8_t)vbyte;
+  // bytes 8 part .. 8 part + 7 of the group's 16: channels 16 apart
+  const uint32_t vw[2] = {four_codes<1>(x, x + 8, vbyte), four_codes<1>(x + 4, x + 12, vbyte)};
   const unsigned long long who = __ballot(ok);
-  const unsigned long long all = TPP * J == 64 ? ~0ull : (1ull << (TPP * J % 64)) - 1;
-  const int place = ((row >> 2) * 16 * J + j) * 4 + (row & 3);   // of byte 0 among this wavefront's bytes; byte r is r J 4 further
-  if (who == all) {   // every byte of this wavefront's rows: in order by way of LDS
-    if (row < TPP) {
+  const int place = ((row >> 2) * 16 * J + 8 * part * J + j) * 4 + (row & 3);   // of the first among this wavefront's bytes; the next is J 4 further
+  if (who == ~0ull) {   // every byte of this wavefront's rows: in order by way of LDS
 #pragma unroll
-      for (int r = 0; r < 16; ++r) codes[wave][place + r * J * 4] = (uint8_t)(vw[r / 4] >> (8 * (r % 4)));
-    }
+    for (int r = 0; r < 8; ++r) codes[wave][place + r * J * 4] = (uint8_t)(vw[r / 4] >> (8 * (r % 4)));
     wave_lds_fence();
-    if (lane < TPP * D / 32)
-      *reinterpret_cast<uint4*>(vcodes + pass * (TPP * D / 2) + lane * 16) = *reinterpret_cast<const uint4*>(&codes[wave][lane * 16]);
+    if (lane < kWaveBytes / 16) *reinterpret_cast<uint4*>(vcodes + lane * 16) = *reinterpret_cast<const uint4*>(&codes[wave][lane * 16]);
   } else if (ok) {
-    uint8_t* const dst = vcodes + pass * (TPP * D / 2) + place;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dst[r * J * 4] = (uint8_t)(vw[r / 4] >> (8 * (r % 4)));
+    for (int r = 0; r < 8; ++r) vcodes[place + r * J * 4] = (uint8_t)(vw[r / 4] >> (8 * (r % 4)));
   }
   if (!kv.meta) return;
   uint32_t there = 0;   // rows that hold a token now
 #pragma unroll
-  for (int i = 0; i < TPP; ++i) there |= (uint32_t)((who >> (i * J)) & 1) << (pass * TPP + i);
+  for (int i = 0; i < TPP; ++i) there |= (uint32_t)((who >> (i * LPT)) & 1) << (pass * TPP + i);
   if constexpr (Work::PASSES == 1) {
     wave_lds_fence();
   } else {
     if (lane == 0) arrived[wave] = there;
     __syncthreads();
-    there = arrived[hl * 2] | arrived[hl * 2 + 1];
     if (pass) return;
+#pragma unroll
+    for (int i = 1; i < Work::PASSES; ++i) there |= arrived[hl * Work::PASSES + i];
   }
   if (h < sh.Hkv) bounds_from_lds<T, D>(keys[hl], there, f.lo, f.hi, f.lo > 0, (T*)kv.meta + tile * 2 * D, lane);
 }
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(256) void read_packed_kernel(KvView kv, Shape sh, c
 
 hipError_t launch_append_packed(hipStream_t st, int dtype, const KvView& kv, const Shape& sh, int batch, int max_new, const NewTokens& in,
                                 const Rotation& rot, const PackedView& out) {
-  const int per_group = sh.g == 32 && sh.d == 128 ? 2 : 4;   // (PageWork::HEADS)
+  const int per_group = 4 * 1024 / (sh.g * sh.d);   // (PageWork::HEADS)
   const dim3 grid(pages_touched(max_new, sh.g), batch, (sh.Hkv + per_group - 1) / per_group);
   auto launch = [&](auto kern) {
     kern<<<grid, 256, 0, st>>>(kv, sh, in, rot, out);
