@@ -1,13 +1,13 @@
 // New tokens into a 4-bit cache, and tokens out of it.
 //
 // Bytes are all there is to them, so what matters is that a wavefront asks for all of its own before it uses any, and stores whole lines.
-// Packing: a lane has one token's group of 32 channels, what a scale is made of, and the 16 bytes that come of it; a wavefront has
-// 16 tokens of a page and head (32 with 64 channels in a page of 32).  Reading: a lane has eight channels of a token, 16 bytes of what is
-// written.  A workgroup is four wavefronts of a page: two halves of two heads, or four heads.
+// Packing: two neighbouring lanes have a token's group of 32 channels, what a scale is made of; a wavefront has 1024 numbers of each of keys and values of a
+// head (8 tokens of 128 channels, 16 of 64).  Reading: a lane has eight channels of a token, 16 bytes of what is written, a wavefront
+// 16 tokens of a head.  A workgroup is four wavefronts of a page.
 //
-// Packing 4 x 4093 tokens (and fewer) of 8 heads of 128, pages of 32, keys turned: 29 us for 88 MB; what the bytes leave is the turning and the
-// latency of three wavefronts a SIMD (angles for 32 channels take 64 registers).  Values a byte at a time: 37 us.  Rows read past the caches: 34, as
-// a lane's 64 bytes are four requests of one line.  Single tokens of 16 sequences: 6 us, four dependent trips to memory.
+// Packing four sequences of 501 to 4093 tokens, 8 heads of 128, pages of 32, keys turned: 22 us for some 80 MB (16 at a large copy's rate); between
+// them are the turning and the latency that five wavefronts a SIMD leave.  A whole group a lane, three wavefronts a SIMD: 27; values a byte at a time as well: 37.
+// Rows read past the caches: 5 more, as a lane's bytes are several requests of one line.  Single tokens of 16 sequences: 5 us, four dependent trips to memory.
 // Reading two sequences of 39012 tokens in all: 26.5 us, 5.3 TB/s (codes and rows past the caches: 29.1 without).
 #include "losa_device.h"
 #include "losa_internal.h"
